@@ -1,0 +1,317 @@
+"""The performance cases of the 8-bit linear layer and the gated feed-forward block.
+
+8-bit rows (the row quantiser that activations and weights go through), the product of 8-bit rows with
+8-bit weights, and the gated feed-forward block act(x Wg^T) * (x Wu^T): on 8-bit rows, on fp16 / bf16
+weights, and its training step (forward and backward).  Shapes are those of LLaMA-7B and LLaMA-70B layers
+(4096 x 11008, 8192 x 28672) and of OPT-125m's 768 x 768 projections; row counts go from one token to
+long prompts and training batches.
+
+``own`` selects what ``run`` computes with: elementary torch operations, or the library's entry points.
+"""
+import math
+
+import torch
+
+own = False
+
+DEV = "cuda"
+_TYPES = {"f16": torch.float16, "bf16": torch.bfloat16, "f32": torch.float32}
+_CODE_MAX = 127.0
+_SCALE_MIN = 2.0 ** -126
+
+
+def _rows(name, m, k, dtype):
+    return {"name": name, "kind": "rows", "m": m, "k": k, "dtype": dtype}
+
+
+def _int8(name, m, n, k, dtype, out):
+    return {"name": name, "kind": "int8", "m": m, "n": n, "k": k, "dtype": dtype, "out": out}
+
+
+def _gated(name, kind, m, f, k, dtype, act):
+    return {"name": name, "kind": kind, "m": m, "f": f, "k": k, "dtype": dtype, "act": act}
+
+
+def listed():
+    return [
+        # The activations of a ragged prompt on the way into an 8-bit down_proj (LLaMA-7B).
+        _rows("rows_7b_ffn_m1500", 1500, 11008, "bf16"),
+        # A LLaMA-70B down_proj weight, one scale per output channel: what loading a model does.
+        _rows("rows_70b_down_weight", 8192, 28672, "f32"),
+        # One token through the smallest projection (OPT-125m q_proj): the call's latency.
+        _int8("int8_opt125m_q_m1", 1, 768, 768, "f16", "f16"),
+        # One token through a LLaMA-70B down_proj: the stream of the weights.
+        _int8("int8_70b_down_m1", 1, 8192, 28672, "bf16", "bf16"),
+        # A ragged short prompt through a LLaMA-7B down_proj, fp32 activations and outputs.
+        _int8("int8_7b_down_m333", 333, 4096, 11008, "f32", "f32"),
+        # A long prompt through a LLaMA-70B up_proj: the largest 8-bit product.
+        _int8("int8_70b_up_m4096", 4096, 28672, 8192, "bf16", "bf16"),
+        # A batch of 64 sequences through a LLaMA-7B feed-forward's first half on 8-bit weights.
+        _gated("gated_int8_7b_m64", "gated_int8", 64, 11008, 4096, "f16", "silu"),
+        # One token through the dense block of LLaMA-7B.
+        _gated("gated_7b_m1", "gated", 1, 11008, 4096, "bf16", "silu"),
+        # A batch of twelve sequences through the dense block of LLaMA-70B.
+        _gated("gated_70b_m12", "gated", 12, 28672, 8192, "f16", "silu"),
+        # A prompt through the dense block of LLaMA-70B.
+        _gated("gated_70b_m2048", "gated", 2048, 28672, 8192, "bf16", "gelu_tanh"),
+        # A training step of a small block of odd sizes on a ragged batch (no row starts aligned).
+        _gated("train_odd_m777", "train", 777, 2731, 1001, "f16", "gelu_tanh"),
+        # A training step of LLaMA-7B's block on 4096 tokens.
+        _gated("train_7b_m4096", "train", 4096, 11008, 4096, "bf16", "silu"),
+    ]
+
+
+def _log(rng, lo, hi):
+    return int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))
+
+
+def _size(rng, lo, hi):
+    """A feature count: mostly a multiple of 64, at times of 8, at times of nothing."""
+    step = rng.choice([64, 64, 64, 8, 1])
+    return max(step, _log(rng, lo, hi) // step * step)
+
+
+def draw(rng):
+    """A case of the same ranges, no larger than the largest listed one of its kind."""
+    kind = rng.choice(["rows", "int8", "int8", "gated_int8", "gated", "gated", "train", "train"])
+    if kind == "rows":
+        k = _size(rng, 64, 28672)
+        return {"kind": kind, "m": _log(rng, 1, min(30000, 8192 * 28672 // k)), "k": k,
+                "dtype": rng.choice(["f16", "bf16", "f32"])}
+    if kind == "int8":
+        n, k = _size(rng, 64, 28672), _size(rng, 64, 28672)
+        top = min(4096, 4096 * 28672 * 8192 // (n * k))
+        m = rng.randint(1, min(16, top)) if rng.random() < 0.4 else _log(rng, 1, top)
+        return {"kind": kind, "m": m, "n": n, "k": k, "dtype": rng.choice(["f16", "bf16", "f32"]),
+                "out": rng.choice(["f16", "bf16", "f32"])}
+    if kind == "train":
+        f, k = _size(rng, 64, 11008), _size(rng, 64, 4096)
+        m = _log(rng, 16, 4096)
+    else:
+        f, k = _size(rng, 64, 28672), _size(rng, 64, 8192)
+        m = rng.randint(1, 16) if rng.random() < 0.4 else _log(rng, 1, 2048)
+    return {"kind": kind, "m": m, "f": f, "k": k, "dtype": rng.choice(["f16", "bf16"]),
+            "act": rng.choice(["silu", "gelu_tanh"])}
+
+
+# ---------------------------------------------------------------------------------------------
+# Inputs
+# ---------------------------------------------------------------------------------------------
+
+def _gen(seed, stream):
+    g = torch.Generator(device=DEV)
+    g.manual_seed((seed * 1000003 + stream * 7919 + 29) % (1 << 62))
+    return g
+
+
+def _activations(g, m, k, dtype):
+    """Gaussian activations of unit size whose columns differ in size, a few of them ten times as large."""
+    col = torch.rand(k, generator=g, device=DEV) + 0.5
+    col = torch.where(torch.rand(k, generator=g, device=DEV) < 0.005, col * 10, col)
+    return (torch.randn(m, k, generator=g, device=DEV) * col).to(_TYPES[dtype])
+
+
+def _weights(g, n, k, dtype):
+    """Gaussian weights of the size that keeps an output near one."""
+    return (torch.randn(n, k, generator=g, device=DEV) * k ** -0.5).to(_TYPES[dtype])
+
+
+def _weight_codes(w):
+    """8-bit codes and a scale per row of an fp32 weight."""
+    s = (w.abs().amax(1) / _CODE_MAX).clamp_min(_SCALE_MIN)
+    return torch.round(w / s[:, None]).to(torch.int8), s
+
+
+def _sdq():
+    import paper_2510_03275_amd as sdq
+    return sdq
+
+
+def _act(sdq, name):
+    return {"silu": sdq.SDQ_ACT_SILU, "gelu_tanh": sdq.SDQ_ACT_GELU_TANH}[name]
+
+
+def _inputs(case, seed):
+    """The tensors of a case by name."""
+    kind, m, k = case["kind"], case["m"], case["k"]
+    t = {"x": _activations(_gen(seed, 1), m, k, case["dtype"])}
+    if kind == "int8":
+        t["wq"], t["ws"] = _weight_codes(_weights(_gen(seed, 2), case["n"], k, "f32"))
+    elif kind == "gated_int8":
+        t["gq"], t["gs"] = _weight_codes(_weights(_gen(seed, 2), case["f"], k, "f32"))
+        t["uq"], t["us"] = _weight_codes(_weights(_gen(seed, 3), case["f"], k, "f32"))
+    elif kind in ("gated", "train"):
+        t["wg"] = _weights(_gen(seed, 2), case["f"], k, case["dtype"])
+        t["wu"] = _weights(_gen(seed, 3), case["f"], k, case["dtype"])
+    if kind == "train":
+        g = _gen(seed, 4)
+        t["dh"] = torch.randn(m, case["f"], generator=g, device=DEV).to(_TYPES[case["dtype"]])
+    return t
+
+
+def prepare(case, seed):
+    st = {"case": case, **_inputs(case, seed)}
+    if not own:
+        return st
+    sdq = _sdq()
+    kind, m, k = case["kind"], case["m"], case["k"]
+    t = _TYPES[case["dtype"]]
+    empty = lambda shape, dtype=t: torch.empty(shape, dtype=dtype, device=DEV)
+    space = lambda nbytes: torch.empty(max(nbytes, 1), dtype=torch.uint8, device=DEV)
+    if kind == "rows":
+        st["out"] = sdq.Int8Rows(empty((m, k), torch.int8), empty(m, torch.float32))
+    elif kind == "int8":
+        st["w"] = sdq.Int8Rows(st["wq"], st["ws"])
+        st["y"] = empty((m, case["n"]), _TYPES[case["out"]])
+        st["workspace"] = space(sdq.sdq_int8_linear_workspace_bytes(m, case["n"], k))
+    elif kind == "gated_int8":
+        st["g8"], st["u8"] = sdq.Int8Rows(st["gq"], st["gs"]), sdq.Int8Rows(st["uq"], st["us"])
+        st["h"] = empty((m, case["f"]))
+        st["workspace"] = space(sdq.sdq_int8_gated_linear_workspace_bytes(m, case["f"], k))
+    else:
+        f = case["f"]
+        st["h"] = empty((m, f))
+        need = sdq.sdq_gated_linear_workspace_bytes(m, f, k)
+        if kind == "train":
+            st["g"], st["u"] = empty((m, f)), empty((m, f))
+            st["dx"], st["dwg"], st["dwu"] = empty((m, k)), empty((f, k)), empty((f, k))
+            need = max(need, sdq.sdq_gated_linear_backward_workspace_bytes(m, f, k))
+        st["workspace"] = space(need)
+    return st
+
+
+# ---------------------------------------------------------------------------------------------
+# One pass
+# ---------------------------------------------------------------------------------------------
+
+def _run_own(st):
+    sdq, case = _sdq(), st["case"]
+    kind = case["kind"]
+    if kind == "rows":
+        r = sdq.int8_quantize(st["x"], out=st["out"])
+        return r.q, r.scales
+    if kind == "int8":
+        return sdq.int8_linear(st["x"], st["w"], workspace=st["workspace"], out=st["y"])
+    act = _act(sdq, case["act"])
+    if kind == "gated_int8":
+        return sdq.int8_gated_linear(st["x"], st["g8"], st["u8"], act, workspace=st["workspace"], out=st["h"])
+    if kind == "gated":
+        return sdq.gated_linear(st["x"], st["wg"], st["wu"], act, workspace=st["workspace"], out=st["h"])
+    h = sdq.gated_linear(st["x"], st["wg"], st["wu"], act, workspace=st["workspace"], out=st["h"],
+                         g=st["g"], u=st["u"])
+    dx, dwg, dwu = sdq.gated_linear_backward(st["dh"], st["x"], st["wg"], st["wu"], st["g"], st["u"], act,
+                                             workspace=st["workspace"], dx=st["dx"], dwg=st["dwg"], dwu=st["dwu"])
+    return h, dx, dwg, dwu
+
+
+def _plain_rows(x):
+    """Codes and scales of rows; the quotients in 64 bits, since codes next to a half must come out right."""
+    s = (x.float().abs().amax(1) / _CODE_MAX).clamp_min(_SCALE_MIN)
+    return torch.round(x.double() / s.double()[:, None]).to(torch.int8), s
+
+
+def _plain_product(q, s, wq, ws):
+    """Products of codes: sums of up to 4e8, which 32 bits do not hold; then both scales."""
+    return (q.double() @ wq.double().t()).float() * (s[:, None] * ws)
+
+
+def _plain_act(g, name):
+    """act(g) and its derivative, from a sigmoid."""
+    if name == "silu":
+        s = 1.0 / (1.0 + torch.exp(-g))
+        return g * s, s * (1.0 + g * (1.0 - s))
+    c = math.sqrt(2.0 / math.pi)
+    t = torch.tanh(c * (g + 0.044715 * g * g * g))
+    return 0.5 * g * (1.0 + t), 0.5 * (1.0 + t) + 0.5 * g * (1.0 - t * t) * c * (1.0 + 0.134145 * g * g)
+
+
+def _run_plain(st):
+    case = st["case"]
+    kind, x = case["kind"], st["x"]
+    if kind == "rows":
+        return _plain_rows(x)
+    if kind == "int8":
+        q, s = _plain_rows(x)
+        return _plain_product(q, s, st["wq"], st["ws"]).to(_TYPES[case["out"]])
+    t = _TYPES[case["dtype"]]
+    if kind == "gated_int8":
+        q, s = _plain_rows(x)
+        a, _ = _plain_act(_plain_product(q, s, st["gq"], st["gs"]), case["act"])
+        return (a * _plain_product(q, s, st["uq"], st["us"])).to(t)
+    xf, wg, wu = x.float(), st["wg"].float(), st["wu"].float()
+    g, u = xf @ wg.t(), xf @ wu.t()
+    a, da = _plain_act(g, case["act"])
+    h = (a * u).to(t)
+    if kind == "gated":
+        return h
+    dh = st["dh"].float()
+    dg, du = dh * u * da, dh * a
+    return h, (dg @ wg + du @ wu).to(t), (dg.t() @ xf).to(t), (du.t() @ xf).to(t)
+
+
+def run(state):
+    return _run_own(state) if own else _run_plain(state)
+
+
+# ---------------------------------------------------------------------------------------------
+# What a pass cannot do without, and the results of the definition
+# ---------------------------------------------------------------------------------------------
+
+def work(case):
+    kind, m, k = case["kind"], case["m"], case["k"]
+    b = _TYPES[case["dtype"]].itemsize
+    if kind == "rows":
+        return {"bytes": m * k * (b + 1) + 4 * m, "flops": 3 * m * k}
+    if kind == "int8":
+        n = case["n"]
+        return {"bytes": m * k * b + n * (k + 4) + m * n * _TYPES[case["out"]].itemsize, "flops": 2 * m * n * k}
+    f = case["f"]
+    if kind == "gated_int8":
+        return {"bytes": m * k * b + 2 * f * (k + 4) + m * f * b, "flops": 4 * m * f * k}
+    if kind == "gated":
+        return {"bytes": b * (m * k + 2 * f * k + m * f), "flops": 4 * m * f * k}
+    # x, dh and the weights in; h, dx and the weights' gradients out
+    return {"bytes": b * (2 * m * k + 4 * f * k + 2 * m * f), "flops": 12 * m * f * k}
+
+
+def _row_codes64(x):
+    x = x.to(torch.float64)
+    scale = torch.clamp((x.abs().max(dim=1).values / 127).to(torch.float32), min=_SCALE_MIN)
+    ratio = x / scale.to(torch.float64).unsqueeze(1)
+    low = torch.floor(ratio)
+    up = (ratio - low > 0.5) | ((ratio - low == 0.5) & (low % 2 != 0))
+    return low + up, scale
+
+
+def exact(case, seed):
+    """The results by the definition, in 64 bits."""
+    t = _inputs(case, seed)
+    kind = case["kind"]
+    if kind == "rows":
+        code, scale = _row_codes64(t["x"])
+        return code.to(torch.int8), scale
+    f64 = torch.float64
+    if kind in ("int8", "gated_int8"):
+        code, scale = _row_codes64(t["x"])
+        left = code * scale.to(f64).unsqueeze(1)
+        weight = lambda q, s: (t[q].to(f64) * t[s].to(f64).unsqueeze(1)).t()
+        if kind == "int8":
+            return torch.mm(left, weight("wq", "ws"))
+        gate, up = torch.mm(left, weight("gq", "gs")), torch.mm(left, weight("uq", "us"))
+    else:
+        left = t["x"].to(f64)
+        gate, up = torch.mm(left, t["wg"].to(f64).t()), torch.mm(left, t["wu"].to(f64).t())
+    if case["act"] == "silu":
+        arg, slope = gate, torch.ones_like(gate)
+    else:
+        c = 2.0 * math.sqrt(2.0 / math.pi)
+        arg, slope = c * (gate + 0.044715 * gate ** 3), c * (1.0 + 3 * 0.044715 * gate ** 2)
+    sig = torch.sigmoid(arg)
+    h = gate * sig * up
+    if kind != "train":
+        return h
+    dh = t["dh"].to(f64)
+    d_up = dh * gate * sig
+    d_gate = dh * up * (sig + gate * sig * torch.sigmoid(-arg) * slope)
+    dx = torch.mm(d_gate, t["wg"].to(f64)) + torch.mm(d_up, t["wu"].to(f64))
+    return h, dx, torch.mm(d_gate.t(), left), torch.mm(d_up.t(), left)
