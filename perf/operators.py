@@ -200,7 +200,8 @@ def _run_own(st):
     h = sdq.gated_linear(st["x"], st["wg"], st["wu"], act, workspace=st["workspace"], out=st["h"],
                          g=st["g"], u=st["u"])
     dx, dwg, dwu = sdq.gated_linear_backward(st["dh"], st["x"], st["wg"], st["wu"], st["g"], st["u"], act,
-                                             workspace=st["workspace"], dx=st["dx"], dwg=st["dwg"], dwu=st["dwu"])
+                                             workspace=st["workspace"], dx=st["dx"], dgate=st["dwg"],
+                                             dup=st["dwu"])
     return h, dx, dwg, dwu
 
 
