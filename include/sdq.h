@@ -387,6 +387,105 @@ sdq_status sdq_linear_expanded(int64_t m, const void* codes_dev, const float* sc
                                void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /*
+ * Dense operators next to the Sigma-Delta linears: layers kept in 8 bits, and
+ * the gated feed-forward block h = act(x Wg^T) * (x Wu^T).
+ *
+ * Every matrix is row-major and densely packed, of any size from one row and
+ * one column on; rows need not start aligned, matrices and workspaces start
+ * 16-byte aligned (else SDQ_ERR_ARG).  m = 0 or n = 0 is a no-op.  Inputs may
+ * hold any values: NaN and infinities go through the formulas of their rows.
+ * Nothing is allocated, synchronised or kept, so every call can be captured
+ * in a graph; calls that share a workspace must be ordered (same stream).
+ * Results are bitwise deterministic.  Sizes whose tiles do not fit one launch
+ * (about 1.7e10 outputs) return SDQ_ERR_SHAPE.
+ */
+
+/* act(g) of the gated block: g / (1 + e^-g), or GELU in its tanh form. */
+typedef enum { SDQ_ACT_SILU = 0, SDQ_ACT_GELU_TANH = 1 } sdq_act;
+
+/*
+ * 8-bit rows (activations per token, weights per output channel):
+ *   scales[i] = max(max_j |x_ij| / 127, 2^-126)   in fp32, rounded once,
+ *   q_ij      = x_ij / scales[i] rounded to the nearest integer, ties to even.
+ * A row with a NaN or an infinity gets the scale NaN and zero codes: whatever
+ * is computed from it is NaN.  x_dev: [m x k] of type xt (F16, BF16, F32);
+ * q_dev: int8 [m x k]; scales_dev: fp32 [m].
+ * Errors: SDQ_ERR_ARG, SDQ_ERR_SHAPE, SDQ_ERR_HIP.
+ */
+sdq_status sdq_int8_quantize(const void* x_dev, sdq_dtype xt, int64_t m, int64_t k, int8_t* q_dev,
+                             float* scales_dev, void* stream);
+
+/*
+ * y_ir = sx_i sw_r sum_j q_ij w_rj: the product of 8-bit rows with 8-bit
+ * weights, summed exactly in 32 bits (k <= 131071, else SDQ_ERR_SHAPE) and
+ * scaled in fp32; rounded once to yt.
+ *   x_dev, xt, x_scales_dev   activations [m x k] of type xt, quantised by the
+ *                call as by sdq_int8_quantize (x_scales_dev NULL); or their
+ *                codes (int8) with their scales, as sdq_int8_quantize left them
+ *                (xt is not read): one quantisation for several linears.
+ *   w_dev, w_scales_dev       int8 [n x k] and fp32 [n].
+ *   y_dev        [m x n] of type yt (F16, BF16 or F32); accumulate nonzero:
+ *                y += the product (the sum is rounded to yt).
+ *   workspace    >= sdq_int8_linear_workspace_bytes(m, n, k) bytes (may be
+ *                NULL where that is 0), no initialisation needed.
+ * Errors: SDQ_ERR_ARG, SDQ_ERR_SHAPE, SDQ_ERR_WORKSPACE, SDQ_ERR_HIP.
+ */
+size_t sdq_int8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k);
+sdq_status sdq_int8_linear(const void* x_dev, sdq_dtype xt, const float* x_scales_dev, int64_t m,
+                           const int8_t* w_dev, const float* w_scales_dev, int64_t n, int64_t k, void* y_dev,
+                           sdq_dtype yt, int32_t accumulate, void* workspace_dev, size_t workspace_bytes,
+                           void* stream);
+
+/*
+ * h = act(g) * u, g and u the 8-bit products of the same rows with gate and up
+ * (int8 [f x k] each, fp32 scales [f]), in one launch after the quantisation;
+ * g, u and the activation are fp32, h [m x f] is rounded once to ht.  Arguments
+ * and errors otherwise as sdq_int8_linear; SDQ_ERR_ARG for an unknown act.
+ */
+size_t sdq_int8_gated_linear_workspace_bytes(int64_t m, int64_t f, int64_t k);
+sdq_status sdq_int8_gated_linear(const void* x_dev, sdq_dtype xt, const float* x_scales_dev, int64_t m,
+                                 const int8_t* gate_dev, const float* gate_scales_dev, const int8_t* up_dev,
+                                 const float* up_scales_dev, int64_t f, int64_t k, int32_t act, void* h_dev,
+                                 sdq_dtype ht, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/*
+ * h = act(g) * u with g = x gate^T, u = x up^T, all of one type t (F16 or BF16;
+ * SDQ_ERR_UNSUPPORTED for F32): x [m x k], gate and up [f x k], h [m x f].
+ * Sums, g, u and the activation are fp32; h is rounded once.
+ *   g_dev, u_dev   both NULL, or [m x f] each: g and u rounded to t, for
+ *                sdq_gated_linear_backward.
+ *   workspace    >= sdq_gated_linear_workspace_bytes(m, f, k) bytes (may be
+ *                NULL where that is 0), no initialisation needed.
+ * Errors: SDQ_ERR_ARG, SDQ_ERR_SHAPE, SDQ_ERR_UNSUPPORTED, SDQ_ERR_WORKSPACE,
+ * SDQ_ERR_HIP.
+ */
+size_t sdq_gated_linear_workspace_bytes(int64_t m, int64_t f, int64_t k);
+sdq_status sdq_gated_linear(const void* x_dev, sdq_dtype t, int64_t m, const void* gate_dev, const void* up_dev,
+                            int64_t f, int64_t k, int32_t act, void* h_dev, void* g_dev, void* u_dev,
+                            void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of the gated block for dh (the gradient of h, [m x f] of type t):
+ *   dg = dh * u * act'(g),  du = dh * act(g)      in fp32, rounded to t,
+ *   dx = dg gate + du up,   dgate = dg^T x,   dup = du^T x     (fp32 sums),
+ * with g and u as sdq_gated_linear wrote them.
+ *   dx_dev       [m x k], or NULL where it is not wanted.
+ *   dgate_dev, dup_dev   [f x k] each, or both NULL (frozen weights; x is not
+ *                read then).  accumulate nonzero: added into them (gradients
+ *                over several batches), the sum rounded to t.
+ *   workspace    >= sdq_gated_linear_backward_workspace_bytes(m, f, k) bytes
+ *                (dg and du among them), no initialisation needed.
+ * m = 0 writes zero gradients of the weights (or leaves them, accumulating),
+ * f = 0 a zero dx.  Errors as sdq_gated_linear.
+ */
+size_t sdq_gated_linear_backward_workspace_bytes(int64_t m, int64_t f, int64_t k);
+sdq_status sdq_gated_linear_backward(const void* dh_dev, const void* x_dev, sdq_dtype t, int64_t m,
+                                     const void* gate_dev, const void* up_dev, int64_t f, int64_t k, int32_t act,
+                                     const void* g_dev, const void* u_dev, void* dx_dev, void* dgate_dev,
+                                     void* dup_dev, int32_t accumulate, void* workspace_dev,
+                                     size_t workspace_bytes, void* stream);
+
+/*
  * MultiOSR (Section 3.4): per-linear OSR from weight variance and size, host
  * only.  Reading of the prose rule: layer OSR proportional to the inverse of
  * the layer's parameter-weighted variance, linear OSR inside a layer

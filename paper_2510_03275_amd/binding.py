@@ -23,6 +23,7 @@ SDQ_F16, SDQ_BF16, SDQ_F32 = 0, 1, 2
 SDQ_HAD_NONE, SDQ_HAD_SYLVESTER, SDQ_HAD_SIGNED = 0, 1, 2
 SDQ_PACK_FIELDS, SDQ_PACK_BASE3 = 0, 1
 SDQ_COMP_GPTQ, SDQ_COMP_JOINT = 0, 1
+SDQ_ACT_SILU, SDQ_ACT_GELU_TANH = 0, 1
 
 STATUS_NAMES = {
     0: "SDQ_OK", -1: "SDQ_ERR_ARG", -2: "SDQ_ERR_SHAPE", -3: "SDQ_ERR_OSR", -4: "SDQ_ERR_LEVELS",
@@ -107,6 +108,21 @@ def _load() -> ctypes.CDLL:
                                         ctypes.c_double, ctypes.c_double, P]),
         "sdq_moments_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64]),
         "sdq_weight_moments": (ctypes.c_int, [P, ctypes.c_int64, P, P, ctypes.c_size_t, P]),
+        "sdq_int8_quantize": (ctypes.c_int, [P, ctypes.c_int, ctypes.c_int64, ctypes.c_int64, P, P, P]),
+        "sdq_int8_linear_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 3),
+        "sdq_int8_linear": (ctypes.c_int, [P, ctypes.c_int, P, ctypes.c_int64, P, P, ctypes.c_int64, ctypes.c_int64,
+                                           P, ctypes.c_int, ctypes.c_int32, P, ctypes.c_size_t, P]),
+        "sdq_int8_gated_linear_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 3),
+        "sdq_int8_gated_linear": (ctypes.c_int, [P, ctypes.c_int, P, ctypes.c_int64, P, P, P, P, ctypes.c_int64,
+                                                 ctypes.c_int64, ctypes.c_int32, P, ctypes.c_int, P,
+                                                 ctypes.c_size_t, P]),
+        "sdq_gated_linear_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 3),
+        "sdq_gated_linear": (ctypes.c_int, [P, ctypes.c_int, ctypes.c_int64, P, P, ctypes.c_int64, ctypes.c_int64,
+                                            ctypes.c_int32, P, P, P, P, ctypes.c_size_t, P]),
+        "sdq_gated_linear_backward_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 3),
+        "sdq_gated_linear_backward": (ctypes.c_int, [P, P, ctypes.c_int, ctypes.c_int64, P, P, ctypes.c_int64,
+                                                     ctypes.c_int64, ctypes.c_int32, P, P, P, P, P, ctypes.c_int32,
+                                                     P, ctypes.c_size_t, P]),
         "sdq_unpack_codes": (ctypes.c_int, [L, P, P]),
         "sdq_upsample_table": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, P]),
         "sdq_prepare": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32]),
@@ -361,6 +377,61 @@ def sdq_weight_moments(w, out, workspace, stream=None) -> None:
                                    workspace.numel() * workspace.element_size(), _stream(stream)))
 
 
+def sdq_int8_quantize(x, q, scales, stream=None) -> None:
+    """Rows of x [m, k] as int8 codes q [m, k] and fp32 scales [m]."""
+    _check(_lib.sdq_int8_quantize(_ptr(x), _dtype_code(x), x.shape[0], x.shape[1], _ptr(q), _ptr(scales),
+                                  _stream(stream)))
+
+
+def sdq_int8_linear_workspace_bytes(m: int, n: int, k: int) -> int:
+    return int(_lib.sdq_int8_linear_workspace_bytes(m, n, k))
+
+
+def sdq_int8_linear(x, w, w_scales, y, workspace, stream=None, accumulate: bool = False, x_scales=None) -> None:
+    """y = x w^T for int8 w [n, k]; x is quantised by the call, or int8 codes with x_scales."""
+    _check(_lib.sdq_int8_linear(_ptr(x), SDQ_F16 if x_scales is not None else _dtype_code(x), _ptr(x_scales),
+                                x.shape[0], _ptr(w), _ptr(w_scales), w.shape[0], w.shape[1], _ptr(y),
+                                _dtype_code(y), int(bool(accumulate)), _ptr(workspace), _nbytes(workspace),
+                                _stream(stream)))
+
+
+def sdq_int8_gated_linear_workspace_bytes(m: int, f: int, k: int) -> int:
+    return int(_lib.sdq_int8_gated_linear_workspace_bytes(m, f, k))
+
+
+def sdq_int8_gated_linear(x, gate, gate_scales, up, up_scales, act: int, h, workspace, stream=None,
+                          x_scales=None) -> None:
+    """h = act(x gate^T) * (x up^T) for int8 gate and up [f, k]; x as in sdq_int8_linear."""
+    _check(_lib.sdq_int8_gated_linear(_ptr(x), SDQ_F16 if x_scales is not None else _dtype_code(x), _ptr(x_scales),
+                                      x.shape[0], _ptr(gate), _ptr(gate_scales), _ptr(up), _ptr(up_scales),
+                                      gate.shape[0], gate.shape[1], int(act), _ptr(h), _dtype_code(h),
+                                      _ptr(workspace), _nbytes(workspace), _stream(stream)))
+
+
+def sdq_gated_linear_workspace_bytes(m: int, f: int, k: int) -> int:
+    return int(_lib.sdq_gated_linear_workspace_bytes(m, f, k))
+
+
+def sdq_gated_linear(x, gate, up, act: int, h, workspace, stream=None, g=None, u=None) -> None:
+    """h = act(x gate^T) * (x up^T), all of x's type; g and u [m, f] also keep the projections."""
+    _check(_lib.sdq_gated_linear(_ptr(x), _dtype_code(x), x.shape[0], _ptr(gate), _ptr(up), gate.shape[0],
+                                 gate.shape[1], int(act), _ptr(h), _ptr(g), _ptr(u), _ptr(workspace),
+                                 _nbytes(workspace), _stream(stream)))
+
+
+def sdq_gated_linear_backward_workspace_bytes(m: int, f: int, k: int) -> int:
+    return int(_lib.sdq_gated_linear_backward_workspace_bytes(m, f, k))
+
+
+def sdq_gated_linear_backward(dh, x, gate, up, act: int, g, u, dx, dgate, dup, workspace, stream=None,
+                              accumulate: bool = False) -> None:
+    """Gradients of sdq_gated_linear for dh; dx may be None, and dgate with dup."""
+    _check(_lib.sdq_gated_linear_backward(_ptr(dh), _ptr(x), _dtype_code(dh), dh.shape[0], _ptr(gate), _ptr(up),
+                                          gate.shape[0], gate.shape[1], int(act), _ptr(g), _ptr(u), _ptr(dx),
+                                          _ptr(dgate), _ptr(dup), int(bool(accumulate)), _ptr(workspace),
+                                          _nbytes(workspace), _stream(stream)))
+
+
 def sdq_unpack_codes(layout: sdq_layout, codes_host: np.ndarray) -> np.ndarray:
     buf = np.ascontiguousarray(codes_host, dtype=np.uint8)
     if buf.size < sdq_codes_bytes(layout):
@@ -488,3 +559,170 @@ def linear(x, enc: Encoded, workspace=None, out=None, stream=None, accumulate: b
     workspace = torch.empty(max(_call_workspace(_addr(layout), m), 1), dtype=torch.uint8, device=x.device)
     sdq_linear(x, enc.codes, enc.scales, layout, y, workspace, stream, accumulate)
     return y
+
+
+@dataclass
+class Int8Rows:
+    q: "object"         # torch.int8 tensor [m, k]
+    scales: "object"    # torch.float32 tensor [m]
+
+
+_HALF = (torch.float16, torch.bfloat16)
+_current_device = torch.cuda.current_device
+
+
+def _matrix(name, t, shape, dtypes) -> None:
+    """t is a dense matrix of that shape on the current device, of one of the types."""
+    if not t.is_cuda or not t.is_contiguous() or t.shape != shape:
+        raise ValueError(f"{name} must be a contiguous device tensor {list(shape)}")
+    if t.dtype not in dtypes:
+        raise ValueError(f"{name} is {t.dtype}, not one of {', '.join(map(str, dtypes))}")
+    if t.device.index != _current_device():
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{_current_device()}")
+
+
+def _rows8(name, r: Int8Rows, shape) -> None:
+    _matrix(name + ".q", r.q, shape, (torch.int8,))
+    _matrix(name + ".scales", r.scales, shape[:1], (torch.float32,))
+
+
+def _rows_in(x, k: int) -> int:
+    """Rows of an activation that is a float matrix or Int8Rows, after its checks."""
+    if isinstance(x, Int8Rows):
+        m = x.q.shape[0] if x.q.dim() == 2 else 0
+        _rows8("x", x, (m, k))
+        return m
+    m = x.shape[0] if x.dim() == 2 else 0
+    _matrix("x", x, (m, k), tuple(_DTYPES))
+    return m
+
+
+def _empty(shape, dtype, device, stream=None):
+    """A tensor whose memory is free for the stream that the call runs on."""
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _workspace(workspace, need: int, device, stream):
+    """The workspace given if it is large enough, else one of the call's own."""
+    if workspace is not None and workspace.nbytes >= need:
+        return workspace
+    return _empty(need, torch.uint8, device, stream) if need else None
+
+
+def int8_quantize(x, out: Optional[Int8Rows] = None, stream=None) -> Int8Rows:
+    """8-bit codes and a scale for every row of a device matrix [m, k] (fp16, bf16 or fp32):
+    activations per token, or weights per output channel."""
+    m, k = x.shape if x.dim() == 2 else (0, 0)
+    _matrix("x", x, (m, k), tuple(_DTYPES))
+    if out is None:
+        out = Int8Rows(_empty((m, k), torch.int8, x.device, stream), _empty((m,), torch.float32, x.device, stream))
+    else:
+        _rows8("out", out, (m, k))
+    sdq_int8_quantize(x, out.q, out.scales, stream)
+    return out
+
+
+def int8_linear(x, w: Int8Rows, workspace=None, out=None, stream=None, accumulate: bool = False, dtype=None):
+    """y = x w^T on 8-bit weights [n, k].
+
+    x is a device matrix [m, k] (fp16, bf16 or fp32), quantised per row by the call, or the
+    Int8Rows of one (int8_quantize), which several linears may share.  y is `out`, or a new
+    tensor of `dtype` (x's type by default; fp16 for Int8Rows).  With accumulate=True the
+    product is added into `out`.  No autograd graph is recorded.
+    """
+    if w.q.dim() != 2:
+        raise ValueError("w.q must be a matrix [n, k]")
+    n, k = w.q.shape
+    _rows8("w", w, (n, k))
+    m = _rows_in(x, k)
+    codes = isinstance(x, Int8Rows)
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate=True needs out")
+        out = _empty((m, n), dtype or (torch.float16 if codes else x.dtype), w.q.device, stream)
+    _matrix("out", out, (m, n), tuple(_DTYPES) if dtype is None else (dtype,))
+    ws = _workspace(workspace, sdq_int8_linear_workspace_bytes(m, n, k), w.q.device, stream)
+    if codes:
+        sdq_int8_linear(x.q, w.q, w.scales, out, ws, stream, accumulate, x.scales)
+    else:
+        sdq_int8_linear(x, w.q, w.scales, out, ws, stream, accumulate)
+    return out
+
+
+def int8_gated_linear(x, gate: Int8Rows, up: Int8Rows, act: int = SDQ_ACT_SILU, workspace=None, out=None,
+                      stream=None, dtype=None):
+    """h = act(x gate^T) * (x up^T) on 8-bit weights [f, k]; x, `out` and `dtype` as in int8_linear."""
+    if gate.q.dim() != 2:
+        raise ValueError("gate.q must be a matrix [f, k]")
+    f, k = gate.q.shape
+    _rows8("gate", gate, (f, k))
+    _rows8("up", up, (f, k))
+    m = _rows_in(x, k)
+    codes = isinstance(x, Int8Rows)
+    if out is None:
+        out = _empty((m, f), dtype or (torch.float16 if codes else x.dtype), gate.q.device, stream)
+    _matrix("out", out, (m, f), tuple(_DTYPES) if dtype is None else (dtype,))
+    ws = _workspace(workspace, sdq_int8_gated_linear_workspace_bytes(m, f, k), gate.q.device, stream)
+    if codes:
+        sdq_int8_gated_linear(x.q, gate.q, gate.scales, up.q, up.scales, act, out, ws, stream, x.scales)
+    else:
+        sdq_int8_gated_linear(x, gate.q, gate.scales, up.q, up.scales, act, out, ws, stream)
+    return out
+
+
+def gated_linear(x, gate, up, act: int = SDQ_ACT_SILU, workspace=None, out=None, stream=None, g=None, u=None):
+    """h = act(x gate^T) * (x up^T) for device matrices x [m, k], gate and up [f, k] of one type
+    (fp16 or bf16).  g and u [m, f], given together, receive the projections, which
+    gated_linear_backward takes.  No autograd graph is recorded."""
+    m, k = x.shape if x.dim() == 2 else (0, 0)
+    f = gate.shape[0] if gate.dim() == 2 else 0
+    t = (x.dtype,)
+    _matrix("x", x, (m, k), _HALF)
+    _matrix("gate", gate, (f, k), t)
+    _matrix("up", up, (f, k), t)
+    for name, v in (("out", out), ("g", g), ("u", u)):
+        if v is not None:
+            _matrix(name, v, (m, f), t)
+    h = out if out is not None else _empty((m, f), x.dtype, x.device, stream)
+    ws = _workspace(workspace, sdq_gated_linear_workspace_bytes(m, f, k), x.device, stream)
+    sdq_gated_linear(x, gate, up, act, h, ws, stream, g, u)
+    return h
+
+
+def gated_linear_backward(dh, x, gate, up, g, u, act: int = SDQ_ACT_SILU, workspace=None, stream=None, dx=None,
+                          dgate=None, dup=None, accumulate: bool = False, need_dx: bool = True,
+                          need_weights: bool = True):
+    """The gradients (dx, dgate, dup) of gated_linear for dh [m, f], with the g and u it kept.
+
+    dx, dgate and dup are written where given, else allocated.  need_dx=False or
+    need_weights=False leaves a part out (None in its place).  With accumulate=True the weights'
+    gradients are added into dgate and dup (which must be given)."""
+    m, k = x.shape if x.dim() == 2 else (0, 0)
+    f = gate.shape[0] if gate.dim() == 2 else 0
+    t = (x.dtype,)
+    _matrix("x", x, (m, k), _HALF)
+    _matrix("gate", gate, (f, k), t)
+    _matrix("up", up, (f, k), t)
+    for name, v in (("dh", dh), ("g", g), ("u", u)):
+        _matrix(name, v, (m, f), t)
+    if accumulate and need_weights and (dgate is None or dup is None):
+        raise ValueError("accumulate=True needs dgate and dup")
+    empty = lambda shape: _empty(shape, x.dtype, x.device, stream)
+    if need_dx:
+        dx = empty((m, k)) if dx is None else dx
+        _matrix("dx", dx, (m, k), t)
+    else:
+        dx = None
+    if need_weights:
+        dgate = empty((f, k)) if dgate is None else dgate
+        dup = empty((f, k)) if dup is None else dup
+        _matrix("dgate", dgate, (f, k), t)
+        _matrix("dup", dup, (f, k), t)
+    else:
+        dgate = dup = None
+    ws = _workspace(workspace, sdq_gated_linear_backward_workspace_bytes(m, f, k), x.device, stream)
+    sdq_gated_linear_backward(dh, x, gate, up, act, g, u, dx, dgate, dup, ws, stream, accumulate)
+    return dx, dgate, dup

@@ -1,0 +1,59 @@
+// Declarations shared by the dense operators: 8-bit rows and their products,
+// and the gated feed-forward block.  Host side in dense_api.cpp.
+#pragma once
+
+#include "sdq_internal.h"
+
+namespace sdq {
+
+// Element types of an operand as the kernels are instantiated.
+enum ElemType { kElemF16 = SDQ_F16, kElemBf16 = SDQ_BF16, kElemI8 = 3 };
+
+// One matrix product of the dense operators,
+//   out[i][r] = sum_c wide(r, c) tall(i, c),   i < rows, r < cols, c < depth,
+// with r the contiguous dimension of the output.  An operand is stored with c
+// contiguous (element (r, c) at r * ld + c) or, `_strided`, with r contiguous
+// (element (r, c) at c * ld + r).
+//
+//   gated        wide[0] and wide[1] are gate and up: both products, then
+//                out = act(g) u.
+//   two sums     segments = 2: out = wide[0] tall[0] + wide[1] tall[1]
+//                (the gradient of the block's input).
+//   two outputs  batch = 2: out[z] = wide[0] tall[z] (the gradients of the two
+//                weights, which share the block's input).
+struct Product {
+  int elem = kElemF16;
+  int64_t rows = 0, cols = 0, depth = 0;
+  const void* wide[2] = {};
+  const void* tall[2] = {};
+  int64_t ld_wide = 0, ld_tall = 0;
+  bool wide_strided = false, tall_strided = false;
+  bool gated = false;
+  int segments = 1, batch = 1;
+  // 8-bit operands: a scale per row of tall and per row of wide
+  const float* tall_scale = nullptr;
+  const float* wide_scale[2] = {};
+  // Output [rows][cols] of type out_type; accumulate: added into.
+  void* out[2] = {};
+  int out_type = SDQ_F16;
+  bool accumulate = false;
+  int act = SDQ_ACT_SILU;
+  void* g_out = nullptr;   // gated: the projections themselves (16-bit, type elem), or NULL
+  void* u_out = nullptr;
+  // partial sums of products split over depth, ws_bytes of them
+  void* ws = nullptr;
+  size_t ws_bytes = 0;
+};
+
+// The workspace launch_product makes use of for this product (ws and ws_bytes not read).
+size_t product_ws_bytes(const Product& p);
+sdq_status launch_product(const Product& p, hipStream_t stream);
+
+sdq_status launch_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, int8_t* q, float* scales,
+                                hipStream_t stream);
+
+// dg = dh u act'(g) and du = dh act(g), rounded to the type t of every operand.
+sdq_status launch_gate_gradient(const void* dh, const void* g, const void* u, sdq_dtype t, int64_t count, int act,
+                                void* dg, void* du, hipStream_t stream);
+
+}  // namespace sdq

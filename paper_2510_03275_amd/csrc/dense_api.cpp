@@ -1,0 +1,313 @@
+// C ABI of the dense operators (include/sdq.h): argument checks, workspace
+// carving and the order of the launches.
+#include <climits>
+
+#include "dense.h"
+
+using namespace sdq;
+
+namespace {
+
+bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+bool float_type(sdq_dtype t) { return t == SDQ_F16 || t == SDQ_BF16 || t == SDQ_F32; }
+bool half_type(sdq_dtype t) { return t == SDQ_F16 || t == SDQ_BF16; }
+bool known_act(int32_t act) { return act == SDQ_ACT_SILU || act == SDQ_ACT_GELU_TANH; }
+
+constexpr int64_t kMaxSize = int64_t{1} << 30;    // rows, cols and depth
+constexpr int64_t kMaxInt8Depth = 131071;         // 128 * 128 * k stays below 2^31
+constexpr int64_t kMaxTiles = int64_t{1} << 23;   // of 32 x 64 outputs: threads of one launch fit 32 bits
+
+sdq_status check_sizes(int64_t m, int64_t n, int64_t k, bool int8) {
+  if (m < 0 || n < 0 || k <= 0)
+    return set_error(SDQ_ERR_ARG, "need m >= 0, n >= 0 and k > 0 (m=%lld n=%lld k=%lld)", (long long)m, (long long)n,
+                     (long long)k);
+  if (int8 && k > kMaxInt8Depth)
+    return set_error(SDQ_ERR_SHAPE, "k=%lld: 8-bit sums are exact in 32 bits up to k = %lld", (long long)k,
+                     (long long)kMaxInt8Depth);
+  if (m > kMaxSize || n > kMaxSize || k > kMaxSize || ((m + 63) / 64) * ((n + 31) / 32) > kMaxTiles ||
+      ((n + 63) / 64) * ((k + 31) / 32) > kMaxTiles || ((m + 63) / 64) * ((k + 31) / 32) > kMaxTiles)
+    return set_error(SDQ_ERR_SHAPE, "m=%lld n=%lld k=%lld is too large for one launch", (long long)m, (long long)n,
+                     (long long)k);
+  return SDQ_OK;
+}
+
+sdq_status check_workspace(size_t need, const void* ws, size_t ws_bytes) {
+  if (need > 0 && (!ws || ws_bytes < need))
+    return set_error(SDQ_ERR_WORKSPACE, "workspace needs %zu bytes, got %zu", need, ws ? ws_bytes : size_t{0});
+  if (!aligned16(ws)) return set_error(SDQ_ERR_ARG, "the workspace must be 16-byte aligned");
+  return SDQ_OK;
+}
+
+// Carves 256-byte aligned pieces; with a NULL base only adds their sizes up.
+struct Carver {
+  char* base;
+  size_t off = 0;
+  void* take(size_t bytes) {
+    const size_t at = off;
+    off = align_up(off + bytes, 256);
+    return base ? base + at : nullptr;
+  }
+};
+
+// The 8-bit product of m rows with one weight, or with gate and up.
+Product int8_product(int64_t m, int64_t n, int64_t k, bool gated) {
+  Product p;
+  p.elem = kElemI8;
+  p.rows = m;
+  p.cols = n;
+  p.depth = p.ld_wide = p.ld_tall = k;
+  p.gated = gated;
+  return p;
+}
+
+struct Int8Space {
+  int8_t* q;
+  float* scales;
+  void* product;
+  size_t product_bytes, bytes;
+};
+Int8Space int8_space(const Product& p, void* ws) {
+  Int8Space s;
+  Carver c{static_cast<char*>(ws)};
+  s.q = static_cast<int8_t*>(c.take(static_cast<size_t>(p.rows) * p.depth));
+  s.scales = static_cast<float*>(c.take(static_cast<size_t>(p.rows) * 4));
+  s.product_bytes = product_ws_bytes(p);
+  s.product = c.take(s.product_bytes);
+  s.bytes = c.off;
+  return s;
+}
+
+size_t int8_bytes(int64_t m, int64_t n, int64_t k, bool gated) {
+  if (check_sizes(m, n, k, true) != SDQ_OK || m == 0 || n == 0) return 0;
+  return int8_space(int8_product(m, n, k, gated), nullptr).bytes;
+}
+
+// Quantises x into the workspace unless it comes as codes, then the product.
+sdq_status run_int8(Product p, const void* x, sdq_dtype xt, const float* x_scales, void* ws, size_t ws_bytes,
+                    hipStream_t stream) {
+  const Int8Space s = int8_space(p, ws);
+  sdq_status st = check_workspace(s.bytes, ws, ws_bytes);
+  if (st != SDQ_OK) return st;
+  if (x_scales) {
+    p.tall[0] = x;
+    p.tall_scale = x_scales;
+  } else {
+    st = launch_int8_quantize(x, xt, p.rows, p.depth, s.q, s.scales, stream);
+    if (st != SDQ_OK) return st;
+    p.tall[0] = s.q;
+    p.tall_scale = s.scales;
+  }
+  p.ws = s.product;
+  p.ws_bytes = s.product_bytes;
+  return launch_product(p, stream);
+}
+
+Product gated_product(sdq_dtype t, int64_t m, int64_t f, int64_t k) {
+  Product p;
+  p.elem = t;
+  p.rows = m;
+  p.cols = f;
+  p.depth = p.ld_wide = p.ld_tall = k;
+  p.gated = true;
+  p.out_type = t;
+  return p;
+}
+
+// dx = dg Wg + du Wu.
+Product input_gradient(sdq_dtype t, int64_t m, int64_t f, int64_t k) {
+  Product p;
+  p.elem = t;
+  p.rows = m;
+  p.cols = k;
+  p.depth = f;
+  p.ld_wide = k;
+  p.ld_tall = f;
+  p.wide_strided = true;
+  p.segments = 2;
+  p.out_type = t;
+  return p;
+}
+
+// dWg = dg^T x, dWu = du^T x.
+Product weight_gradient(sdq_dtype t, int64_t m, int64_t f, int64_t k) {
+  Product p;
+  p.elem = t;
+  p.rows = f;
+  p.cols = k;
+  p.depth = m;
+  p.ld_wide = k;
+  p.ld_tall = f;
+  p.wide_strided = p.tall_strided = true;
+  p.batch = 2;
+  p.out_type = t;
+  return p;
+}
+
+struct BackwardSpace {
+  void *dg, *du, *product;
+  size_t product_bytes, bytes;
+};
+BackwardSpace backward_space(sdq_dtype t, int64_t m, int64_t f, int64_t k, void* ws) {
+  BackwardSpace s;
+  Carver c{static_cast<char*>(ws)};
+  const size_t bytes = static_cast<size_t>(m) * f * 2;
+  s.dg = c.take(bytes);
+  s.du = c.take(bytes);
+  const size_t a = product_ws_bytes(input_gradient(t, m, f, k)), b = product_ws_bytes(weight_gradient(t, m, f, k));
+  s.product_bytes = a > b ? a : b;
+  s.product = c.take(s.product_bytes);
+  s.bytes = c.off;
+  return s;
+}
+
+}  // namespace
+
+extern "C" {
+
+sdq_status sdq_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, int8_t* q, float* scales,
+                             void* stream) {
+  if (!float_type(xt)) return set_error(SDQ_ERR_ARG, "bad dtype");
+  if (m < 0 || k <= 0) return set_error(SDQ_ERR_ARG, "need m >= 0 and k > 0");
+  if (m > kMaxTiles || k > kMaxSize) return set_error(SDQ_ERR_SHAPE, "m=%lld k=%lld is too large for one launch",
+                                                      (long long)m, (long long)k);
+  if (m == 0) return SDQ_OK;
+  if (!x || !q || !scales) return set_error(SDQ_ERR_ARG, "NULL pointer argument");
+  if (!aligned16(x) || !aligned16(q)) return set_error(SDQ_ERR_ARG, "x and q must be 16-byte aligned");
+  return launch_int8_quantize(x, xt, m, k, q, scales, static_cast<hipStream_t>(stream));
+}
+
+size_t sdq_int8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k) { return int8_bytes(m, n, k, false); }
+
+sdq_status sdq_int8_linear(const void* x, sdq_dtype xt, const float* x_scales, int64_t m, const int8_t* w,
+                           const float* w_scales, int64_t n, int64_t k, void* y, sdq_dtype yt, int32_t accumulate,
+                           void* ws, size_t ws_bytes, void* stream) {
+  if (!float_type(yt) || (!x_scales && !float_type(xt))) return set_error(SDQ_ERR_ARG, "bad dtype");
+  sdq_status st = check_sizes(m, n, k, true);
+  if (st != SDQ_OK || m == 0 || n == 0) return st;
+  if (!x || !w || !w_scales || !y) return set_error(SDQ_ERR_ARG, "NULL pointer argument");
+  if (!aligned16(x) || !aligned16(w) || !aligned16(y))
+    return set_error(SDQ_ERR_ARG, "x, w and y must be 16-byte aligned");
+  Product p = int8_product(m, n, k, false);
+  p.wide[0] = w;
+  p.wide_scale[0] = w_scales;
+  p.out[0] = y;
+  p.out_type = yt;
+  p.accumulate = accumulate != 0;
+  return run_int8(p, x, xt, x_scales, ws, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+size_t sdq_int8_gated_linear_workspace_bytes(int64_t m, int64_t f, int64_t k) { return int8_bytes(m, f, k, true); }
+
+sdq_status sdq_int8_gated_linear(const void* x, sdq_dtype xt, const float* x_scales, int64_t m, const int8_t* gate,
+                                 const float* gate_scales, const int8_t* up, const float* up_scales, int64_t f,
+                                 int64_t k, int32_t act, void* h, sdq_dtype ht, void* ws, size_t ws_bytes,
+                                 void* stream) {
+  if (!float_type(ht) || (!x_scales && !float_type(xt))) return set_error(SDQ_ERR_ARG, "bad dtype");
+  if (!known_act(act)) return set_error(SDQ_ERR_ARG, "act %d is not an sdq_act", act);
+  sdq_status st = check_sizes(m, f, k, true);
+  if (st != SDQ_OK || m == 0 || f == 0) return st;
+  if (!x || !gate || !gate_scales || !up || !up_scales || !h) return set_error(SDQ_ERR_ARG, "NULL pointer argument");
+  if (!aligned16(x) || !aligned16(gate) || !aligned16(up) || !aligned16(h))
+    return set_error(SDQ_ERR_ARG, "x, gate, up and h must be 16-byte aligned");
+  Product p = int8_product(m, f, k, true);
+  p.wide[0] = gate;
+  p.wide[1] = up;
+  p.wide_scale[0] = gate_scales;
+  p.wide_scale[1] = up_scales;
+  p.out[0] = h;
+  p.out_type = ht;
+  p.act = act;
+  return run_int8(p, x, xt, x_scales, ws, ws_bytes, static_cast<hipStream_t>(stream));
+}
+
+size_t sdq_gated_linear_workspace_bytes(int64_t m, int64_t f, int64_t k) {
+  if (check_sizes(m, f, k, false) != SDQ_OK || m == 0 || f == 0) return 0;
+  return product_ws_bytes(gated_product(SDQ_F16, m, f, k));
+}
+
+sdq_status sdq_gated_linear(const void* x, sdq_dtype t, int64_t m, const void* gate, const void* up, int64_t f,
+                            int64_t k, int32_t act, void* h, void* g, void* u, void* ws, size_t ws_bytes,
+                            void* stream) {
+  if (!float_type(t)) return set_error(SDQ_ERR_ARG, "bad dtype");
+  if (!half_type(t)) return set_error(SDQ_ERR_UNSUPPORTED, "the dense block takes fp16 or bf16");
+  if (!known_act(act)) return set_error(SDQ_ERR_ARG, "act %d is not an sdq_act", act);
+  sdq_status st = check_sizes(m, f, k, false);
+  if (st != SDQ_OK || m == 0 || f == 0) return st;
+  if (!x || !gate || !up || !h) return set_error(SDQ_ERR_ARG, "NULL pointer argument");
+  if (!g != !u) return set_error(SDQ_ERR_ARG, "g and u are given together or not at all");
+  if (!aligned16(x) || !aligned16(gate) || !aligned16(up) || !aligned16(h) || !aligned16(g) || !aligned16(u))
+    return set_error(SDQ_ERR_ARG, "x, gate, up, h, g and u must be 16-byte aligned");
+  Product p = gated_product(t, m, f, k);
+  p.ws = ws;
+  p.ws_bytes = product_ws_bytes(p);
+  st = check_workspace(p.ws_bytes, ws, ws_bytes);
+  if (st != SDQ_OK) return st;
+  p.tall[0] = x;
+  p.wide[0] = gate;
+  p.wide[1] = up;
+  p.out[0] = h;
+  p.g_out = g;
+  p.u_out = u;
+  p.act = act;
+  return launch_product(p, static_cast<hipStream_t>(stream));
+}
+
+size_t sdq_gated_linear_backward_workspace_bytes(int64_t m, int64_t f, int64_t k) {
+  if (check_sizes(m, f, k, false) != SDQ_OK) return 0;
+  return backward_space(SDQ_F16, m, f, k, nullptr).bytes;
+}
+
+sdq_status sdq_gated_linear_backward(const void* dh, const void* x, sdq_dtype t, int64_t m, const void* gate,
+                                     const void* up, int64_t f, int64_t k, int32_t act, const void* g, const void* u,
+                                     void* dx, void* dgate, void* dup, int32_t accumulate, void* ws, size_t ws_bytes,
+                                     void* stream) {
+  if (!float_type(t)) return set_error(SDQ_ERR_ARG, "bad dtype");
+  if (!half_type(t)) return set_error(SDQ_ERR_UNSUPPORTED, "the dense block takes fp16 or bf16");
+  if (!known_act(act)) return set_error(SDQ_ERR_ARG, "act %d is not an sdq_act", act);
+  sdq_status st = check_sizes(m, f, k, false);
+  if (st != SDQ_OK) return st;
+  if (!dgate != !dup) return set_error(SDQ_ERR_ARG, "dgate and dup are given together or not at all");
+  if (m > 0 && f > 0 && (!dh || !g || !u)) return set_error(SDQ_ERR_ARG, "NULL pointer argument");
+  if ((dx && m > 0 && f > 0 && (!gate || !up)) || (dgate && m > 0 && f > 0 && !x))
+    return set_error(SDQ_ERR_ARG, "NULL pointer argument");
+  for (const void* q : {dh, x, gate, up, g, u, static_cast<const void*>(dx), static_cast<const void*>(dgate),
+                        static_cast<const void*>(dup)})
+    if (!aligned16(q)) return set_error(SDQ_ERR_ARG, "tensors must be 16-byte aligned");
+  const BackwardSpace s = backward_space(t, m, f, k, ws);
+  st = check_workspace(s.bytes, ws, ws_bytes);
+  if (st != SDQ_OK) return st;
+  const hipStream_t hs = static_cast<hipStream_t>(stream);
+  if (!dx && !dgate) return SDQ_OK;
+  if (m > 0 && f > 0) {
+    st = launch_gate_gradient(dh, g, u, t, m * f, act, s.dg, s.du, hs);
+    if (st != SDQ_OK) return st;
+  }
+  // Without rows or features the sums are empty: the products write zeros.
+  if (dx && m > 0) {
+    Product p = input_gradient(t, m, f, k);
+    p.wide[0] = gate;
+    p.wide[1] = up;
+    p.tall[0] = s.dg;
+    p.tall[1] = s.du;
+    p.out[0] = dx;
+    p.ws = s.product;
+    p.ws_bytes = s.product_bytes;
+    st = launch_product(p, hs);
+    if (st != SDQ_OK) return st;
+  }
+  if (dgate && f > 0) {
+    Product p = weight_gradient(t, m, f, k);
+    p.wide[0] = x;
+    p.tall[0] = s.dg;
+    p.tall[1] = s.du;
+    p.out[0] = dgate;
+    p.out[1] = dup;
+    p.accumulate = accumulate != 0;
+    p.ws = s.product;
+    p.ws_bytes = s.product_bytes;
+    st = launch_product(p, hs);
+  }
+  return st;
+}
+
+}  // extern "C"
