@@ -405,7 +405,7 @@ typedef enum { SDQ_ACT_SILU = 0, SDQ_ACT_GELU_TANH = 1 } sdq_act;
 
 /*
  * 8-bit rows (activations per token, weights per output channel):
- *   scales[i] = max(max_j |x_ij| / 127, 2^-126)   in fp32, rounded once,
+ *   scales[i] = max(c max_j |x_ij|, 2^-126)   in fp32, c = fp32(1 / 127),
  *   q_ij      = x_ij / scales[i] rounded to the nearest integer, ties to even.
  * A row with a NaN or an infinity gets the scale NaN and zero codes: whatever
  * is computed from it is NaN.  x_dev: [m x k] of type xt (F16, BF16, F32);

@@ -49,6 +49,9 @@ struct Product {
 size_t product_ws_bytes(const Product& p);
 sdq_status launch_product(const Product& p, hipStream_t stream);
 
+// The product on 256 x 256 tiles: rows aligned as launch_product checks it.
+void launch_wide(const Product& p, hipStream_t stream);
+
 sdq_status launch_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, int8_t* q, float* scales,
                                 hipStream_t stream);
 

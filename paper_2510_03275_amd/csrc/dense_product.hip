@@ -203,8 +203,17 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict_
 
 size_t product_ws_bytes(const Product&) { return 0; }
 
+// Whether every 16 bytes that a tile reads of either operand lie in one row and start aligned,
+// and 128 rows' offsets fit 31 bits.
+static bool rows_aligned(const Product& p) {
+  const int64_t b = p.elem == kElemI8 ? 1 : 2;
+  if (p.ld_wide * b % 16 || p.ld_tall * b % 16) return false;
+  return std::max(p.ld_wide, p.ld_tall) * b <= (int64_t{1} << 23) && p.depth > 0 && p.depth <= (int64_t{1} << 29);
+}
+
 sdq_status launch_product(const Product& p, hipStream_t stream) {
-  if (p.elem == kElemF16) launch_any<kElemF16>(p, stream);
+  if (rows_aligned(p) && p.rows > 128) launch_wide(p, stream);
+  else if (p.elem == kElemF16) launch_any<kElemF16>(p, stream);
   else if (p.elem == kElemBf16) launch_any<kElemBf16>(p, stream);
   else launch_any<kElemI8>(p, stream);
   const hipError_t e = hipGetLastError();

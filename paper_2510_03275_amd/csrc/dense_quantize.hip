@@ -1,5 +1,5 @@
-// 8-bit rows: per row the scale s = max(a / 127, 2^-126) of its largest
-// magnitude a (fp32, one rounding), then q = x / s rounded to nearest, ties to
+// 8-bit rows: per row the scale s = max(a c, 2^-126) of its largest
+// magnitude a (c = fp32(1 / 127); one rounding), then q = x / s rounded to nearest, ties to
 // even, of the exact quotient.  A row that holds a NaN or an infinity gets the
 // scale NaN and zero codes, so that everything computed from it is NaN.
 //
@@ -52,7 +52,7 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const S* __restrict_
   a = __builtin_elementwise_maximum(__builtin_elementwise_maximum(part[0], part[1]),
                                     __builtin_elementwise_maximum(part[2], part[3]));
   const bool finite = a <= 3.4028234663852886e38f;
-  const float s = fmaxf(a / 127.0f, 0x1p-126f);
+  const float s = fmaxf(a * (1.0f / 127.0f), 0x1p-126f);
   const float inv = 1.0f / s;
   if (tid == 0) scales[row] = finite ? s : __builtin_nanf("");
   for (int64_t c = tid * kPer; c < whole; c += 256 * kPer) {

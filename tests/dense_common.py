@@ -32,7 +32,7 @@ def floor(t):
 def quantize_ref(x):
     """Codes (int64) and fp32 scales of the rows of x, by the definition."""
     x = x.double()
-    s = (x.abs().amax(1).float() / 127.0).clamp_min(2.0 ** -126)
+    s = (x.abs().amax(1).float() * torch.tensor(1 / 127, dtype=torch.float32)).clamp_min(2.0 ** -126)
     ok = torch.isfinite(x).all(1)
     t = x / s.double()[:, None]
     q = torch.where(ok[:, None], torch.round(t), torch.zeros_like(t))   # ties to even
