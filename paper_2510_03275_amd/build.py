@@ -25,7 +25,7 @@ ARCH = os.environ.get("SDQ_OFFLOAD_ARCH", "gfx950")
 SOURCES = ["sdq_api.cpp", "encoder.hip", "linear_decode.hip", "linear_prefill.hip", "expand_prefill.hip",
            "prefill_digits.hip",
            "moments.hip", "compensation.hip", "linear_noalloc.hip",
-           "dense_api.cpp", "dense_product.hip", "dense_wide.hip", "dense_quantize.hip"]
+           "dense_api.cpp", "dense_product.hip", "dense_wide.hip", "dense_few.hip", "dense_quantize.hip"]
 
 COMMON = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
