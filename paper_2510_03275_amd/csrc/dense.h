@@ -49,7 +49,7 @@ struct Product {
 size_t product_ws_bytes(const Product& p);
 sdq_status launch_product(const Product& p, hipStream_t stream);
 
-// At most 16 rows, neither operand strided.
+// At most 64 rows, neither operand strided.
 void launch_few(const Product& p, hipStream_t stream);
 // The product on 256 x 256 tiles: rows aligned as launch_product checks it.
 void launch_wide(const Product& p, hipStream_t stream);

@@ -212,7 +212,7 @@ static bool rows_aligned(const Product& p) {
 }
 
 sdq_status launch_product(const Product& p, hipStream_t stream) {
-  if (p.rows <= 16 && !p.wide_strided) launch_few(p, stream);
+  if (p.rows <= 64 && !p.wide_strided) launch_few(p, stream);
   else if (rows_aligned(p) && p.rows > 128) launch_wide(p, stream);
   else if (p.elem == kElemF16) launch_any<kElemF16>(p, stream);
   else if (p.elem == kElemBf16) launch_any<kElemBf16>(p, stream);
