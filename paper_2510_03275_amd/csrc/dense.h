@@ -51,7 +51,14 @@ sdq_status launch_product(const Product& p, hipStream_t stream);
 
 // At most 64 rows, neither operand strided.
 void launch_few(const Product& p, hipStream_t stream);
-// The product on 256 x 256 tiles: rows aligned as launch_product checks it.
+// The product on tiles of 256 rows of wide (dense_wide.hip), rows aligned as launch_product
+// checks it: how many rows of tall to a tile, and into how many parts the depth is cut, whose
+// sums take wide_part_bytes of the workspace.
+struct WidePlan {
+  int tall = 256, splits = 0;
+};
+WidePlan wide_plan(const Product& p);
+size_t wide_part_bytes(const Product& p, int splits);
 void launch_wide(const Product& p, hipStream_t stream);
 
 sdq_status launch_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, int8_t* q, float* scales,

@@ -110,4 +110,26 @@ __device__ inline f32x4 scaled4(const i32x4& a, float st, const float* sw, int64
   return v;
 }
 
+// Four outputs r .. r + 3 of row i from their sums (GATED: a of gate, b of up).
+template <int ELEM, bool GATED>
+__device__ inline void finish4(const Product& p, int z, int64_t i, int64_t r, const typename Elem<ELEM>::Acc& a,
+                               const typename Elem<ELEM>::Acc& b) {
+  const float st = ELEM == kElemI8 ? p.tall_scale[i] : 1.0f;
+  const f32x4 g = scaled4(a, st, p.wide_scale[0], r, p.cols);
+  if constexpr (!GATED) {
+    store4(p.out[z], i, r, p.cols, p.out_type, p.accumulate, g);
+    return;
+  } else {
+    const f32x4 u = scaled4(b, st, p.wide_scale[1], r, p.cols);
+    f32x4 h;
+#pragma unroll
+    for (int v = 0; v < 4; ++v) h[v] = act_value(g[v], p.act) * u[v];
+    store4(p.out[0], i, r, p.cols, p.out_type, false, h);
+    if (p.g_out) {
+      store4(p.g_out, i, r, p.cols, p.elem, false, g);
+      store4(p.u_out, i, r, p.cols, p.elem, false, u);
+    }
+  }
+}
+
 }  // namespace sdq

@@ -118,21 +118,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Product p) {
     const int t = o % kColTiles, j = o / kColTiles;
     const int64_t row = 16 * j + lane % 16, r = col0 + 16 * t + 4 * (lane / 16);
     if (row >= p.rows || r >= p.cols) continue;
-    const float st = ELEM == kElemI8 ? p.tall_scale[row] : 1.0f;
-    const f32x4 g = scaled4(part[0][t][j][lane], st, p.wide_scale[0], r, p.cols);
-    if constexpr (GATED) {
-      const f32x4 u = scaled4(part[0][kColTiles + t][j][lane], st, p.wide_scale[1], r, p.cols);
-      f32x4 h;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) h[v] = act_value(g[v], p.act) * u[v];
-      store4(p.out[0], row, r, p.cols, p.out_type, false, h);
-      if (p.g_out) {
-        store4(p.g_out, row, r, p.cols, p.elem, false, g);
-        store4(p.u_out, row, r, p.cols, p.elem, false, u);
-      }
-    } else {
-      store4(p.out[0], row, r, p.cols, p.out_type, p.accumulate, g);
-    }
+    finish4<ELEM, GATED>(p, 0, row, r, part[0][t][j][lane], part[0][GATED ? kColTiles + t : t][j][lane]);
   }
 }
 

@@ -201,8 +201,6 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict_
 
 }  // namespace
 
-size_t product_ws_bytes(const Product&) { return 0; }
-
 // Whether every 16 bytes that a tile reads of either operand lie in one row and start aligned,
 // and 128 rows' offsets fit 31 bits.
 static bool rows_aligned(const Product& p) {
@@ -211,9 +209,14 @@ static bool rows_aligned(const Product& p) {
   return std::max(p.ld_wide, p.ld_tall) * b <= (int64_t{1} << 23) && p.depth > 0 && p.depth <= (int64_t{1} << 29);
 }
 
+size_t product_ws_bytes(const Product& p) {
+  if (p.rows <= 64 && !p.wide_strided) return 0;
+  return rows_aligned(p) ? 1 << 28 : 0;
+}
+
 sdq_status launch_product(const Product& p, hipStream_t stream) {
-  if (p.rows <= 64 && !p.wide_strided) launch_few(p, stream);
-  else if (rows_aligned(p) && p.rows > 128) launch_wide(p, stream);
+  if (p.rows <= (getenv("FEW") ? atoi(getenv("FEW")) : 64) && !p.wide_strided) launch_few(p, stream);
+  else if (rows_aligned(p)) launch_wide(p, stream);
   else if (p.elem == kElemF16) launch_any<kElemF16>(p, stream);
   else if (p.elem == kElemBf16) launch_any<kElemBf16>(p, stream);
   else launch_any<kElemI8>(p, stream);

@@ -1,7 +1,7 @@
-// The products of the dense operators on 256 x 256 tiles (dense.h), for operands
-// whose rows start 16-byte aligned.
+// The products of the dense operators on tiles of 256 rows of wide by 256, 128
+// or 64 rows of tall (dense.h), for operands whose rows start 16-byte aligned.
 //
-// What bounds it: a step of 128 bytes of depth takes 64 matrix-core
+// What bounds it, at 256 x 256: a step of 128 bytes of depth takes 64 matrix-core
 // instructions per wave (two waves per SIMD: 2048 clocks per step), 192 KB of LDS
 // reads (1536 clocks at 128 bytes) and 64 KB of copies into LDS.  So the
 // matrix cores and LDS have to run side by side, and nothing may wait for memory:
@@ -29,6 +29,13 @@
 //             elements); a group of 16 lanes reads 4 depths x 16 elements
 //             transposed (ds_read_b64_tr_b16), 32-byte granule p of depth c at
 //             p ^ (c % 4 + 4 (c / 8 % 2)).
+//   outputs   The sums go through LDS, half a tile at a time, so that the stores are
+//             whole rows and the code that scales, activates and converts exists once
+//             (unrolled over a lane's 128 sums it was 130 KB of instructions, whose
+//             first fetch took 20 us).
+//   splits    Where the tiles are fewer than the compute units, the depth is cut and
+//             the sums of every part go to the workspace; join_kernel adds them in
+//             order.
 //   ends      Buffer resources end with the operand: rows past its end read as
 //             zeros, as do depths past its end (for depth-contiguous rows, whose
 //             neighbours follow, the lanes past the end get an address out of range).
@@ -48,7 +55,7 @@ typedef __attribute__((address_space(3))) void* LdsPtr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* LdsS4;
 
-constexpr int kQuarter = 16384, kHalfRows = 128, kBuf = 4 * kQuarter;
+constexpr int kWideHalf = 16384;            // bytes of half a tile's rows of wide, one step
 constexpr unsigned kOut = 0x80000000u;      // an offset past every buffer
 constexpr int kRsrcWord3 = 0x00020000;
 
@@ -69,8 +76,12 @@ struct Quarter {
   int left;                  // bytes of depth left (depth-contiguous)
 };
 
-template <int BYTES, bool STRIDED>
+// ROWS: of a half.  A wave issues kCopies copies per step and half (of 32 rows, waves 4-7
+// repeat those of waves 0-3).
+template <int BYTES, bool STRIDED, int ROWS>
 struct Copier {
+  static_assert(!STRIDED || ROWS == 128, "strided halves hold 128 rows");
+  static constexpr int kCopies = ROWS == 128 ? 2 : 1;
   int64_t step;              // bytes from one step to the next
   int depth_bytes;
   unsigned off[2];           // the lane's two source offsets
@@ -87,39 +98,41 @@ struct Copier {
       chunk = 0;
     } else {
       chunk = 16 * ((lane % 8) ^ (lane / 8));
-      off[0] = (8 * wave + lane / 8) * ld_bytes + chunk;
+      off[0] = (8 * (ROWS == 32 ? wave % 4 : wave) + lane / 8) * ld_bytes + chunk;
       off[1] = off[0] + 64 * ld_bytes;
     }
   }
-  // Rows r0 .. of n rows (r0 may lie past them: nothing is read then).
+  // Rows r0 .. of n rows (r0 may lie past them: nothing is read then) from step t on; steps per segment.
   __device__ inline Quarter quarter(const void* first, const void* second, int64_t r0, int64_t n, int64_t ld,
-                                    int64_t depth) const {
+                                    int64_t depth, int t, int steps) const {
     Quarter q;
     const int64_t at = r0 * (STRIDED ? 1 : ld) * BYTES;
-    q.src = static_cast<const char*>(first) + at;
+    q.src = static_cast<const char*>(t < steps ? first : second) + at;
     q.second = static_cast<const char*>(second) + at;
     // Rows behind a strided operand's last one belong to the next depth: they are read, and
     // their outputs not stored.
     const int64_t valid = n - r0;
-    q.bytes0 = STRIDED ? ((depth - 1) * ld + valid) * BYTES : (valid < kHalfRows ? valid : kHalfRows) * ld * BYTES;
+    q.bytes0 = STRIDED ? (depth * ld - r0) * BYTES : (valid < ROWS ? valid : ROWS) * ld * BYTES;
     if (valid <= 0) q.bytes0 = 0;
-    q.bytes = q.bytes0;
-    q.left = depth_bytes;
+    const int past = t < steps ? t : t - steps;
+    q.src += past * step;
+    q.bytes = q.bytes0 - past * step;
+    q.left = depth_bytes - 128 * past;
     return q;
   }
-  // The next step of q to LDS.  Past the last one the offsets are out of range: zeros.
-  __device__ inline void copy(Quarter& q, char* lds, int wave) const {
+  // The next step of q to LDS, zeros unless `read`.
+  __device__ inline void copy(Quarter& q, char* lds, int wave, bool read) const {
     unsigned o0 = off[0], o1 = off[1];
     if (!STRIDED) {
       const bool past = chunk >= q.left;
       o0 = past ? kOut : o0;
       o1 = past ? kOut : o1;
     }
-    const int num = q.bytes <= 0 ? 0 : q.bytes < 0x7FFFFFFF ? static_cast<int>(q.bytes) : 0x7FFFFFFF;
+    const int num = !read || q.bytes <= 0 ? 0 : q.bytes < 0x7FFFFFFF ? static_cast<int>(q.bytes) : 0x7FFFFFFF;
     const __amdgpu_buffer_rsrc_t rs =
         __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(q.src), static_cast<short>(0), num, kRsrcWord3);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + wave * 1024), 16, o0, 0, 0, 0);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + 8192 + wave * 1024), 16, o1, 0, 0, 0);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + (ROWS == 32 ? wave % 4 : wave) * 1024), 16, o0, 0, 0, 0);
+    if (kCopies == 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + 8192 + wave * 1024), 16, o1, 0, 0, 0);
     q.src += step;
     q.bytes -= step;
     q.left -= 128;
@@ -164,11 +177,15 @@ struct Places {
 
 constexpr int kXcds = 8;
 
-template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED>
-__global__ __launch_bounds__(512, 2) void wide_kernel(Product p) {
+template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED, int TALL>
+__global__ __launch_bounds__(512, TALL == 64 ? 4 : 2) void wide_kernel(Product p, int splits) {
   using E = Elem<ELEM>;
   using Acc = typename E::Acc;
   constexpr int kB = E::kBytes, kStep = 128 / kB;
+  constexpr int kHalf = TALL / 2, kWaveRows = kHalf / 2, kFrags = kWaveRows / 16;
+  constexpr int kTallHalf = kHalf * 128, kBuf = 2 * kTallHalf + 2 * kWideHalf;
+  using CopyA = Copier<kB, TALL_STRIDED, kHalf>;
+  using CopyB = Copier<kB, WIDE_STRIDED, 128>;
   __shared__ __attribute__((aligned(1024))) char lds[2 * kBuf];   // [step % 2][A0, A1, B0, B1]
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
@@ -177,48 +194,53 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p) {
   // The tile.
   constexpr int kCols = GATED ? 128 : 256;
   const unsigned nw = static_cast<unsigned>((p.cols + kCols - 1) / kCols);
-  const unsigned nt = static_cast<unsigned>((p.rows + 255) / 256);
+  const unsigned nt = static_cast<unsigned>((p.rows + TALL - 1) / TALL);
   const unsigned total = gridDim.x, id = blockIdx.x;
   const unsigned xcd = id % kXcds, per = total / kXcds, rem = total % kXcds;
   unsigned tile = xcd * per + (xcd < rem ? xcd : rem) + id / kXcds;
-  const int z = __builtin_amdgcn_readfirstlane(tile / (nw * nt));
-  tile -= z * (nw * nt);
+  const int part = __builtin_amdgcn_readfirstlane(tile / (nw * nt));     // of the batch, or of the depth
+  tile -= part * (nw * nt);
+  const int z = splits > 1 ? 0 : part;
   const unsigned band = tile / (4 * nw), in_band = tile - band * (4 * nw);
   const unsigned band_rows = nt - 4 * band < 4 ? nt - 4 * band : 4;
   const unsigned tw = in_band / band_rows, tt = 4 * band + (in_band - tw * band_rows);
-  const int64_t row0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(tt)) * 256;
+  const int64_t row0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(tt)) * TALL;
   const int64_t col0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(tw)) * kCols;
 
-  Copier<kB, TALL_STRIDED> ca;
-  Copier<kB, WIDE_STRIDED> cb;
+  const int seg_steps = static_cast<int>((p.depth + kStep - 1) / kStep), steps = seg_steps * p.segments;
+  const int each = steps / splits, more = steps % splits, at = splits > 1 ? part : 0;
+  const int t0 = at * each + min(at, more), t1 = t0 + each + (at < more ? 1 : 0);
+
+  CopyA ca;
+  CopyB cb;
   ca.init(p.ld_tall, p.depth, wave, lane);
   cb.init(p.ld_wide, p.depth, wave, lane);
   Quarter qa[2], qb[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    qa[h] = ca.quarter(p.tall[p.batch > 1 ? z : 0], p.tall[1], row0 + kHalfRows * h, p.rows, p.ld_tall, p.depth);
-    qb[h] = cb.quarter(p.wide[GATED ? h : 0], p.wide[1], GATED ? col0 : col0 + kHalfRows * h, p.cols, p.ld_wide,
-                       p.depth);
+    qa[h] = ca.quarter(p.tall[p.batch > 1 ? z : 0], p.tall[1], row0 + kHalf * h, p.rows, p.ld_tall, p.depth, t0,
+                       seg_steps);
+    qb[h] = cb.quarter(p.wide[GATED ? h : 0], p.wide[1], GATED ? col0 : col0 + 128 * h, p.cols, p.ld_wide, p.depth, t0,
+                       seg_steps);
   }
-  const int seg_steps = static_cast<int>((p.depth + kStep - 1) / kStep), steps = seg_steps * p.segments;
 
   Places<TALL_STRIDED> pa;
   Places<WIDE_STRIDED> pb;
-  pa.init(64 * wt, lane);
+  pa.init(kWaveRows * wt, lane);
   pb.init(32 * ww, lane);
 
   // Step t of half h to its place: A (tall) or B (wide).
   auto copy_a = [&](int h, int t) {
-    if (t == seg_steps && p.segments > 1) ca.next_segment(qa[h]);
-    ca.copy(qa[h], lds + (t % 2) * kBuf + h * kQuarter, wave);
+    if (t == seg_steps && t0 < seg_steps && p.segments > 1) ca.next_segment(qa[h]);
+    ca.copy(qa[h], lds + ((t - t0) % 2) * kBuf + h * kTallHalf, wave, t < t1);
   };
   auto copy_b = [&](int h, int t) {
-    if (t == seg_steps && p.segments > 1) cb.next_segment(qb[h]);
-    cb.copy(qb[h], lds + (t % 2) * kBuf + (2 + h) * kQuarter, wave);
+    if (t == seg_steps && t0 < seg_steps && p.segments > 1) cb.next_segment(qb[h]);
+    cb.copy(qb[h], lds + ((t - t0) % 2) * kBuf + 2 * kTallHalf + h * kWideHalf, wave, t < t1);
   };
 
-  Acc acc[2][2][4][2] = {};       // [A half][B half][rows of tall / 16][rows of wide / 16]
-  i32x4 a[4][2], b[2][2][2];      // A half: [rows / 16][depth half]; B: [half][rows / 16][depth half]
+  Acc acc[2][2][kFrags][2] = {};  // [A half][B half][rows of tall / 16][rows of wide / 16]
+  i32x4 a[kFrags][2], b[2][2][2];      // A half: [rows / 16][depth half]; B: [half][rows / 16][depth half]
 
   auto multiply = [&](int ha, int hb) {
     barrier();
@@ -226,7 +248,7 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p) {
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < kFrags; ++i)
 #pragma unroll
         for (int j = 0; j < 2; ++j) acc[ha][hb][i][j] = E::mfma(b[hb][j][s], a[i][s], acc[ha][hb][i][j]);
     __builtin_amdgcn_s_setprio(0);
@@ -234,7 +256,7 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p) {
   };
   auto read_a = [&](const char* q) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < kFrags; ++i)
 #pragma unroll
       for (int s = 0; s < 2; ++s) a[i][s] = pa.read(q, i, s);
   };
@@ -246,11 +268,11 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p) {
   };
   auto wait = [&]() {
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(wait_counts(12));
+    __builtin_amdgcn_s_waitcnt(wait_counts(6 + 3 * CopyA::kCopies));   // the last six quarters
     asm volatile("" ::: "memory");
   };
 
-  for (int t = 0; t < 2; ++t) {
+  for (int t = t0; t < t0 + 2; ++t) {
     copy_b(0, t);
     copy_a(0, t);
     copy_b(1, t);
@@ -258,94 +280,156 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p) {
   }
   wait();
   barrier();
-  read_b(lds + 2 * kQuarter, 0);
+  read_b(lds + 2 * kTallHalf, 0);
   wait();
   barrier();
   if (wt == 1) barrier();
 
-  for (int t = 0; t < steps; ++t) {
-    const char* cur = lds + (t % 2) * kBuf;
-    const char* nxt = lds + ((t + 1) % 2) * kBuf;
+  for (int t = t0; t < t1; ++t) {
+    const char* cur = lds + ((t - t0) % 2) * kBuf;
+    const char* nxt = lds + ((t - t0 + 1) % 2) * kBuf;
     read_a(cur);
     copy_b(0, t + 2);
     wait();
     multiply(0, 0);
-    read_b(cur + 3 * kQuarter, 1);
+    read_b(cur + 2 * kTallHalf + kWideHalf, 1);
     copy_a(0, t + 2);
     wait();
     multiply(0, 1);
-    read_a(cur + kQuarter);
+    read_a(cur + kTallHalf);
     copy_b(1, t + 2);
     wait();
     multiply(1, 0);
-    read_b(nxt + 2 * kQuarter, 0);
+    read_b(nxt + 2 * kTallHalf, 0);
     copy_a(1, t + 2);
     wait();
     multiply(1, 1);
   }
   if (wt == 0) barrier();
-  __builtin_amdgcn_s_waitcnt(0);      // no copy lands after the workgroup's LDS is released
+  __builtin_amdgcn_s_waitcnt(0);      // the copies past the end land before the sums take their place
+  __syncthreads();
 
+  // Sums of half a tile: [kHalf rows][64 chunks of four columns], chunk q of row r at q ^ (r % 16).
+  // Chunks 0-31 are of B0, 32-63 of B1.
+  Acc* sums = reinterpret_cast<Acc*>(lds);
+  const int64_t ld_part = (p.cols + 3) / 4 * 4;      // of gate and of up
 #pragma unroll
-  for (int ha = 0; ha < 2; ++ha)
+  for (int ha = 0; ha < 2; ++ha) {
+    if (ha) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t row = row0 + kHalfRows * ha + 64 * wt + 16 * i + lane % 16;
-      if (row >= p.rows) continue;
-      const float st = ELEM == kElemI8 ? p.tall_scale[row] : 1.0f;
+    for (int hb = 0; hb < 2; ++hb)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) {
-        const int64_t r0 = col0 + 32 * ww + 16 * j + 4 * (lane / 16);
-        if constexpr (GATED) {
-          if (r0 >= p.cols) continue;
-          const f32x4 g = scaled4(acc[ha][0][i][j], st, p.wide_scale[0], r0, p.cols);
-          const f32x4 u = scaled4(acc[ha][1][i][j], st, p.wide_scale[1], r0, p.cols);
-          f32x4 h;
+      for (int i = 0; i < kFrags; ++i)
 #pragma unroll
-          for (int v = 0; v < 4; ++v) h[v] = act_value(g[v], p.act) * u[v];
-          store4(p.out[0], row, r0, p.cols, p.out_type, false, h);
-          if (p.g_out) {
-            store4(p.g_out, row, r0, p.cols, p.elem, false, g);
-            store4(p.u_out, row, r0, p.cols, p.elem, false, u);
-          }
-        } else {
-#pragma unroll
-          for (int hb = 0; hb < 2; ++hb) {
-            const int64_t r = r0 + kHalfRows * hb;
-            if (r >= p.cols) continue;
-            store4(p.out[z], row, r, p.cols, p.out_type, p.accumulate,
-                   scaled4(acc[ha][hb][i][j], st, p.wide_scale[0], r, p.cols));
-          }
+        for (int j = 0; j < 2; ++j) {
+          const int r = kWaveRows * wt + 16 * i + lane % 16, q = 32 * hb + 8 * ww + 4 * j + lane / 16;
+          sums[r * 64 + (q ^ (r % 16))] = acc[ha][hb][i][j];
         }
+    __syncthreads();
+    if (splits > 1) {
+#pragma unroll 2
+      for (int o = tid; o < kHalf * 64; o += 512) {
+        const int r = o / 64, q = o % 64;
+        const int64_t row = row0 + kHalf * ha + r, c = col0 + 4 * (GATED ? q % 32 : q);
+        if (row >= p.rows || c >= p.cols) continue;
+        Acc* dst = static_cast<Acc*>(p.ws) + (part * p.rows + row) * ((GATED ? 2 : 1) * ld_part / 4) +
+                   (GATED ? q / 32 : 0) * (ld_part / 4) + c / 4;
+        *dst = sums[r * 64 + (q ^ (r % 16))];
       }
+      continue;
     }
+    constexpr int kOuts = GATED ? 32 : 64;
+#pragma unroll 2
+    for (int o = tid; o < kHalf * kOuts; o += 512) {
+      const int r = o / kOuts, q = o % kOuts;
+      const int64_t row = row0 + kHalf * ha + r, c = col0 + 4 * q;
+      if (row >= p.rows || c >= p.cols) continue;
+      finish4<ELEM, GATED>(p, z, row, c, sums[r * 64 + (q ^ (r % 16))],
+                           GATED ? sums[r * 64 + ((q + 32) ^ (r % 16))] : Acc{});
+    }
+  }
 }
 
-template <int ELEM, bool WS, bool TS, bool GATED>
-void launch_tiles(const Product& p, hipStream_t stream) {
+// Adds the parts of a split product in order: one thread per four outputs.
+template <int ELEM, bool GATED>
+__global__ __launch_bounds__(256) void join_kernel(Product p, int splits) {
+  using Acc = typename Elem<ELEM>::Acc;
+  const int64_t quads = (p.cols + 3) / 4, o = blockIdx.x * int64_t{256} + threadIdx.x;
+  if (o >= quads * p.rows) return;
+  const int64_t row = o / quads, q = o - row * quads, ld = (GATED ? 2 : 1) * quads;
+  const Acc* src = static_cast<const Acc*>(p.ws) + row * ld + q;
+  Acc a = {}, b = {};
+  for (int s = 0; s < splits; ++s) {
+    a += src[s * p.rows * ld];
+    if (GATED) b += src[s * p.rows * ld + quads];
+  }
+  finish4<ELEM, GATED>(p, 0, row, 4 * q, a, b);
+}
+
+template <int ELEM, bool WS, bool TS, bool GATED, int TALL>
+void launch_tiles(const Product& p, int splits, hipStream_t stream) {
   const int64_t per = GATED ? 128 : 256;
-  const int64_t tiles = (p.cols + per - 1) / per * ((p.rows + 255) / 256) * p.batch;
-  wide_kernel<ELEM, WS, TS, GATED><<<dim3(static_cast<unsigned>(tiles)), 512, 0, stream>>>(p);
+  const int64_t tiles = (p.cols + per - 1) / per * ((p.rows + TALL - 1) / TALL);
+  wide_kernel<ELEM, WS, TS, GATED, TALL>
+      <<<dim3(static_cast<unsigned>(tiles * p.batch * splits)), 512, 0, stream>>>(p, splits);
+  if (splits > 1) {
+    const int64_t quads = (p.cols + 3) / 4 * p.rows;
+    join_kernel<ELEM, GATED><<<dim3(static_cast<unsigned>((quads + 255) / 256)), 256, 0, stream>>>(p, splits);
+  }
+}
+
+template <int ELEM, bool WS, bool GATED>
+void launch_tall(const Product& p, const WidePlan& plan, hipStream_t stream) {
+  if (plan.tall == 64) launch_tiles<ELEM, WS, false, GATED, 64>(p, plan.splits, stream);
+  else if (plan.tall == 128) launch_tiles<ELEM, WS, false, GATED, 128>(p, plan.splits, stream);
+  else launch_tiles<ELEM, WS, false, GATED, 256>(p, plan.splits, stream);
 }
 
 template <int ELEM>
-void launch_elem(const Product& p, hipStream_t stream) {
-  if (p.gated) return launch_tiles<ELEM, false, false, true>(p, stream);
-  if constexpr (ELEM == kElemI8) {
-    launch_tiles<ELEM, false, false, false>(p, stream);
-  } else if (p.tall_strided) {
-    launch_tiles<ELEM, true, true, false>(p, stream);
-  } else {
-    launch_tiles<ELEM, true, false, false>(p, stream);
-  }
+void launch_elem(const Product& p, const WidePlan& plan, hipStream_t stream) {
+  if (p.gated) return launch_tall<ELEM, false, true>(p, plan, stream);
+  if constexpr (ELEM == kElemI8) launch_tall<ELEM, false, false>(p, plan, stream);
+  else if (p.tall_strided) launch_tiles<ELEM, true, true, false, 256>(p, plan.splits, stream);
+  else launch_tall<ELEM, true, false>(p, plan, stream);
 }
 
 }  // namespace
 
+size_t wide_part_bytes(const Product& p, int splits) {
+  return splits > 1 ? static_cast<size_t>(p.rows) * ((p.cols + 3) / 4) * 16 * (p.gated ? 2 : 1) * splits : 0;
+}
+
+WidePlan wide_plan(const Product& p) {
+  const int64_t bytes = p.elem == kElemI8 ? 1 : 2;
+  const int64_t steps = (p.depth * bytes + 127) / 128 * p.segments, units = device_compute_units();
+  const int64_t col_tiles = (p.cols + (p.gated ? 127 : 255)) / (p.gated ? 128 : 256);
+  WidePlan best;
+  double best_us = 0;
+  for (int tall = 256; tall >= (p.tall_strided ? 256 : 64); tall /= 2) {
+    const int64_t tiles = col_tiles * ((p.rows + tall - 1) / tall) * p.batch;
+    const int64_t at_once = tall == 64 ? 2 * units : units;
+    const double step_us = tall == 256 ? 0.95 : tall == 128 ? 0.6 : 0.9, fixed_us = tall == 256 ? 6 : 4;
+    for (int splits = 1; splits <= (p.batch > 1 ? 1 : 32) && (splits == 1 || steps / splits >= 4); ++splits) {
+      const int64_t turns = (tiles * splits + at_once - 1) / at_once;
+      const double us = turns * (fixed_us + ((steps + splits - 1) / splits) * step_us) +
+                        (splits > 1 ? 3.0 + wide_part_bytes(p, splits) * 2e-6 / 4.0 : 0.0);
+      if (best.splits == 0 || us < best_us) {
+        best.tall = tall;
+        best.splits = splits;
+        best_us = us;
+      }
+    }
+  }
+  return best;
+}
+
 void launch_wide(const Product& p, hipStream_t stream) {
-  if (p.elem == kElemF16) launch_elem<kElemF16>(p, stream);
-  else if (p.elem == kElemBf16) launch_elem<kElemBf16>(p, stream);
-  else launch_elem<kElemI8>(p, stream);
+  WidePlan plan = wide_plan(p);
+  if (const char* f = getenv("WIDE_FORCE")) sscanf(f, "%d,%d", &plan.tall, &plan.splits);
+  while (plan.splits > 1 && wide_part_bytes(p, plan.splits) > p.ws_bytes) --plan.splits;
+  if (p.elem == kElemF16) launch_elem<kElemF16>(p, plan, stream);
+  else if (p.elem == kElemBf16) launch_elem<kElemBf16>(p, plan, stream);
+  else launch_elem<kElemI8>(p, plan, stream);
 }
 
 }  // namespace sdq
