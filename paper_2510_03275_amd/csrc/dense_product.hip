@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict_
 static bool rows_aligned(const Product& p) {
   const int64_t b = p.elem == kElemI8 ? 1 : 2;
   if (p.ld_wide * b % 16 || p.ld_tall * b % 16) return false;
-  return std::max(p.ld_wide, p.ld_tall) * b <= (int64_t{1} << 23) && p.depth > 0 && p.depth <= (int64_t{1} << 29);
+  return std::max(p.ld_wide, p.ld_tall) * b < (int64_t{1} << 23) && p.depth > 0 && p.depth <= (int64_t{1} << 29);
 }
 
 size_t product_ws_bytes(const Product& p) {

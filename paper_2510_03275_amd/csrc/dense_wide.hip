@@ -240,72 +240,113 @@ __global__ __launch_bounds__(512, TALL == 64 ? 4 : 2) void wide_kernel(Product p
   };
 
   Acc acc[2][2][kFrags][2] = {};  // [A half][B half][rows of tall / 16][rows of wide / 16]
-  i32x4 a[kFrags][2], b[2][2][2];      // A half: [rows / 16][depth half]; B: [half][rows / 16][depth half]
+  i32x4 a[2][kFrags][2], b[2][2][2];   // halves: [rows / 16][depth half]
 
+#ifndef VAR
+#define VAR 0
+#endif
+#define VPRIO (VAR & 1)
+#define VILV (VAR & 2)
+#define VTWO (VAR & 4)
   auto multiply = [&](int ha, int hb) {
-    barrier();
-    __builtin_amdgcn_s_setprio(1);
+    if (!VILV) __builtin_amdgcn_sched_barrier(0);
+    if (VPRIO) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int s = 0; s < 2; ++s)
 #pragma unroll
       for (int i = 0; i < kFrags; ++i)
 #pragma unroll
-        for (int j = 0; j < 2; ++j) acc[ha][hb][i][j] = E::mfma(b[hb][j][s], a[i][s], acc[ha][hb][i][j]);
-    __builtin_amdgcn_s_setprio(0);
-    barrier();
+        for (int j = 0; j < 2; ++j) acc[ha][hb][i][j] = E::mfma(b[hb][j][s], a[ha][i][s], acc[ha][hb][i][j]);
+    if (VPRIO) __builtin_amdgcn_s_setprio(0);
+    if (VILV) {
+#pragma unroll
+      for (int n = 0; n < 8; ++n) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x008, kFrags / 2 ? kFrags / 2 : 1, 0);
+      }
+    }
+    if (!VTWO) __builtin_amdgcn_sched_barrier(0);
   };
-  auto read_a = [&](const char* q) {
+  auto read_a = [&](const char* buf, int h) {
 #pragma unroll
     for (int i = 0; i < kFrags; ++i)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) a[i][s] = pa.read(q, i, s);
+      for (int s = 0; s < 2; ++s) a[h][i][s] = pa.read(buf + h * kTallHalf, i, s);
   };
-  auto read_b = [&](const char* q, int h) {
+  auto read_b = [&](const char* buf, int h) {
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) b[h][j][s] = pb.read(q, j, s);
+      for (int s = 0; s < 2; ++s) b[h][j][s] = pb.read(buf + 2 * kTallHalf + h * kWideHalf, j, s);
   };
-  auto wait = [&]() {
+  // The end of a phase: what was read has arrived, and the quarter read next, of every wave.
+  auto turn = [&]() {
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(wait_counts(6 + 3 * CopyA::kCopies));   // the last six quarters
+    __builtin_amdgcn_s_waitcnt(wait_counts(6 + 3 * CopyA::kCopies));   // all but the last six quarters
     asm volatile("" ::: "memory");
+    barrier();
   };
 
   for (int t = t0; t < t0 + 2; ++t) {
-    copy_b(0, t);
     copy_a(0, t);
+    copy_b(0, t);
     copy_b(1, t);
     copy_a(1, t);
   }
-  wait();
-  barrier();
-  read_b(lds + 2 * kTallHalf, 0);
-  wait();
-  barrier();
-  if (wt == 1) barrier();
+  turn();
+  read_a(lds, 0);
+  read_b(lds, 0);
+  turn();
+  copy_a(0, t0 + 2);
+  turn();
 
+#if VAR & 4
+  auto turn2 = [&]() {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(wait_counts(4 + 2 * CopyA::kCopies));
+    asm volatile("" ::: "memory");
+    barrier();
+  };
   for (int t = t0; t < t1; ++t) {
     const char* cur = lds + ((t - t0) % 2) * kBuf;
     const char* nxt = lds + ((t - t0 + 1) % 2) * kBuf;
-    read_a(cur);
+    read_b(cur, 1);
     copy_b(0, t + 2);
-    wait();
     multiply(0, 0);
-    read_b(cur + 2 * kTallHalf + kWideHalf, 1);
-    copy_a(0, t + 2);
-    wait();
+    read_a(cur, 1);
+    if (t > t0) copy_a(0, t + 2);
     multiply(0, 1);
-    read_a(cur + kTallHalf);
+    turn2();
+    read_a(nxt, 0);
     copy_b(1, t + 2);
-    wait();
     multiply(1, 0);
-    read_b(nxt + 2 * kTallHalf, 0);
+    read_b(nxt, 0);
     copy_a(1, t + 2);
-    wait();
     multiply(1, 1);
+    turn2();
   }
-  if (wt == 0) barrier();
+#else
+  for (int t = t0; t < t1; ++t) {
+    const char* cur = lds + ((t - t0) % 2) * kBuf;
+    const char* nxt = lds + ((t - t0 + 1) % 2) * kBuf;
+    read_b(cur, 1);
+    copy_b(0, t + 2);
+    multiply(0, 0);
+    turn();
+    read_a(cur, 1);
+    copy_b(1, t + 2);
+    multiply(0, 1);
+    turn();
+    read_a(nxt, 0);
+    copy_a(1, t + 2);
+    multiply(1, 0);
+    turn();
+    read_b(nxt, 0);
+    copy_a(0, t + 3);
+    multiply(1, 1);
+    turn();
+  }
+#endif
   __builtin_amdgcn_s_waitcnt(0);      // the copies past the end land before the sums take their place
   __syncthreads();
 
@@ -427,6 +468,18 @@ void launch_wide(const Product& p, hipStream_t stream) {
   WidePlan plan = wide_plan(p);
   if (const char* f = getenv("WIDE_FORCE")) sscanf(f, "%d,%d", &plan.tall, &plan.splits);
   while (plan.splits > 1 && wide_part_bytes(p, plan.splits) > p.ws_bytes) --plan.splits;
+  if (plan.tall == 256) {
+    launch_big(p, plan.splits, stream);
+    if (plan.splits > 1) {
+      const int64_t quads = (p.cols + 3) / 4 * p.rows;
+      const dim3 grid(static_cast<unsigned>((quads + 255) / 256));
+      if (p.elem == kElemI8 && p.gated) join_kernel<kElemI8, true><<<grid, 256, 0, stream>>>(p, plan.splits);
+      else if (p.elem == kElemI8) join_kernel<kElemI8, false><<<grid, 256, 0, stream>>>(p, plan.splits);
+      else if (p.gated) join_kernel<kElemF16, true><<<grid, 256, 0, stream>>>(p, plan.splits);
+      else join_kernel<kElemF16, false><<<grid, 256, 0, stream>>>(p, plan.splits);
+    }
+    return;
+  }
   if (p.elem == kElemF16) launch_elem<kElemF16>(p, plan, stream);
   else if (p.elem == kElemBf16) launch_elem<kElemBf16>(p, plan, stream);
   else launch_elem<kElemI8>(p, plan, stream);
