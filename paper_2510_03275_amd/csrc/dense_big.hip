@@ -14,17 +14,16 @@ typedef __attribute__((address_space(3))) void* LdsPtr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* LdsS4;
 
-constexpr int kStepBytes = 64;                 // of depth
+constexpr int kStepBytes = 128;                // of depth
 constexpr int kOperand = 256 * kStepBytes;     // bytes of one operand's step in LDS
-constexpr int kStage = 2 * kOperand;
-constexpr int kStages = 5;
+constexpr int kTallStages = 2, kWideStages = 3;
 constexpr unsigned kOut = 0x80000000u;         // an offset past every buffer
 constexpr int kRsrcWord3 = 0x00020000;
 constexpr int kXcds = 8;
 
 constexpr int wait_counts(int vm) { return (vm & 15) | ((vm >> 4) << 14) | (7 << 4); }   // and lgkmcnt(0)
 
-// The copies of a workgroup's 256 rows of an operand, one step after the other: two per wave and
+// The copies of a workgroup's 256 rows of an operand, one step after the other: four per wave and
 // step.  Depth-contiguous: the descriptors stay (of two halves for gate and up) and the step is the
 // scalar offset.  Strided: the descriptor moves, and ends with the depth.  Scalars that are compared
 // are 32 bits wide: no branch splits the loop.
@@ -38,8 +37,8 @@ struct Loader {
   int soff;                  // depth-contiguous: bytes of the steps done
   int depth, left;           // of the segment: in bytes (depth-contiguous) or depths
   int row_bytes, skip;       // strided: of one depth, and in front of the rows
-  unsigned off[2];           // the lane's source offsets
-  int chunk;                 // its place in a step's 64 bytes (depth-contiguous)
+  unsigned off[4];           // the lane's source offsets
+  int chunk;                 // its place in a step's 128 bytes (depth-contiguous)
 
   // Rows r0 .. of n rows, from step t on; steps per segment.
   __device__ inline void init(const void* first, const void* other, int64_t r0, int64_t n, int64_t ld, int64_t depth_,
@@ -49,7 +48,7 @@ struct Loader {
     const int64_t at = r0 * (STRIDED ? 1 : ld) * BYTES;
     const int valid = static_cast<int>(n) - static_cast<int>(r0);
     if (STRIDED) {
-      // LDS: [half][32 depths][128 elements]: copy j of wave w holds depths 4 w .. 4 w + 3 of half j
+      // LDS: [half][64 depths][128 elements]: copy j of wave w holds depths 4 (w + 8 (j % 2)) .. + 3 of half j / 2
       depth = static_cast<int>(depth_);
       step = kStep * static_cast<int64_t>(ld_bytes);
       src[0] = static_cast<const char*>(t < steps ? first : other) + at + past * step;
@@ -58,11 +57,11 @@ struct Loader {
       skip = static_cast<int>(r0) * BYTES;
       const int swz = ((lane / 16) << 1) | (wave / 2 % 2);
       const int r = (((lane % 16) / 2) ^ swz) * 16 + (lane % 2) * 8;
-      for (int j = 0; j < 2; ++j) off[j] = (4 * wave + lane / 16) * ld_bytes + 2 * (r + 128 * j);
+      for (int j = 0; j < 4; ++j) off[j] = (4 * wave + lane / 16 + 32 * (j % 2)) * ld_bytes + 2 * (r + 128 * (j / 2));
       left = depth - past * kStep;
       chunk = soff = 0;
     } else {
-      // LDS: [256 rows][64 bytes]: copy j of wave w holds rows 16 (w + 8 j) .. + 15
+      // LDS: [256 rows][128 bytes]: copy j of wave w holds rows 8 (w + 8 j) .. + 7
       depth = static_cast<int>(depth_ * BYTES);
       src[0] = static_cast<const char*>(t < steps ? first : other) + at;
       second = static_cast<const char*>(other) + at;
@@ -71,8 +70,8 @@ struct Loader {
         src[HALVES] = second;
         num[HALVES] = num[0];
       }
-      chunk = 16 * ((lane % 4) ^ (lane / 16));
-      for (int j = 0; j < 2; ++j) off[j] = (16 * wave + lane / 4 + (HALVES ? 0 : 128 * j)) * ld_bytes + chunk;
+      chunk = 16 * ((lane % 8) ^ (lane / 8));
+      for (int j = 0; j < 4; ++j) off[j] = (8 * wave + lane / 8 + 64 * (HALVES ? j % 2 : j)) * ld_bytes + chunk;
       soff = past * kStepBytes;
       left = depth - soff;
       row_bytes = skip = 0;
@@ -89,8 +88,8 @@ struct Loader {
     }
     const int have = MASK && !read ? 0 : left;
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      const int h = HALVES ? j : 0;
+    for (int j = 0; j < 4; ++j) {
+      const int h = HALVES ? j / 2 : 0;
       // Strided: columns behind the operand's last belong to the next depth: they are read, and their
       // outputs not stored.
       const int end = STRIDED ? max(min(have, kStep) * row_bytes - skip, 0) : num[h];
@@ -109,7 +108,7 @@ struct Loader {
 // The lane's places in an operand's step for a wave's 16 N rows from row0 on.
 template <bool STRIDED, int N>
 struct Frags {
-  int at[STRIDED ? N : 1];
+  int at[STRIDED ? N : 2];
   __device__ inline void init(int row0, int lane) {
     const int g = lane / 16, i = lane % 16;
     if (STRIDED) {
@@ -118,18 +117,18 @@ struct Frags {
         at[n] = row0 / 128 * (kOperand / 2) + (8 * g + i / 4) * 256 + granule * 32 + (i % 4) * 8;
       }
     } else {
-      at[0] = (row0 + i) * kStepBytes + ((g ^ (i / 4)) * 16);
+      for (int s = 0; s < 2; ++s) at[s] = (row0 + i) * kStepBytes + (((4 * s + g) ^ (i % 8)) * 16);
     }
   }
-  // Fragment n (16 rows).
-  __device__ inline i32x4 read(const char* lds, int n) const {
+  // Fragment n (16 rows) of depth half s.
+  __device__ inline i32x4 read(const char* lds, int n, int s) const {
     if constexpr (STRIDED) {
-      const char* p = lds + at[n];
+      const char* p = lds + at[n] + s * 8192;
       const s16x4 lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4)p);
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4)(p + 1024));
       return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      return *reinterpret_cast<const i32x4*>(lds + at[0] + n * 16 * kStepBytes);
+      return *reinterpret_cast<const i32x4*>(lds + at[s] + n * 16 * kStepBytes);
     }
   }
 };
@@ -139,7 +138,7 @@ __global__ __launch_bounds__(512, 2) void big_kernel(Product p, int splits) {
   using E = Elem<ELEM>;
   using Acc = typename E::Acc;
   constexpr int kB = E::kBytes, kStep = kStepBytes / kB;
-  __shared__ __attribute__((aligned(1024))) char lds[kStages * kStage];   // [stage][tall, wide]
+  __shared__ __attribute__((aligned(1024))) char lds[(kTallStages + kWideStages) * kOperand];   // stages of tall, of wide
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int ww = wave % 4, wt = wave / 4;
@@ -173,75 +172,89 @@ __global__ __launch_bounds__(512, 2) void big_kernel(Product p, int splits) {
   fa.init(128 * wt, lane);
   fb.init(64 * ww, lane);
 
-  int put = 0, get = 0;      // the stages (as LDS offsets) written and read next
-  auto copy = [&](int t, auto mask) {
-    const bool restart = kSegments && t == seg_steps && t0 < seg_steps;
-    la.template copy<decltype(mask)::value, kSegments>(lds + put, wave, t < t1, restart);
-    lb.template copy<decltype(mask)::value, kSegments>(lds + put + kOperand, wave, t < t1, restart);
-    put = put + kStage == kStages * kStage ? 0 : put + kStage;
+  // LDS offsets of the stages read and filled next.
+  constexpr int kWide = kTallStages * kOperand, kEnd = kWide + kWideStages * kOperand;
+  int get_a = 0, get_b = kWide, put_a = 0, put_b = kWide;
+  auto next_a = [](int at) { return at + kOperand == kWide ? 0 : at + kOperand; };
+  auto next_b = [](int at) { return at + kOperand == kEnd ? kWide : at + kOperand; };
+  auto restart = [&](int t) { return kSegments && t == seg_steps && t0 < seg_steps; };
+  auto copy_a = [&](int t, auto mask) {
+    la.template copy<decltype(mask)::value, kSegments>(lds + put_a, wave, t < t1, restart(t));
+    put_a = next_a(put_a);
+  };
+  auto copy_b = [&](int t, auto mask) {
+    lb.template copy<decltype(mask)::value, kSegments>(lds + put_b, wave, t < t1, restart(t));
+    put_b = next_b(put_b);
   };
 
   Acc acc[8][4] = {};        // [rows of tall / 16][rows of wide / 16]
-  i32x4 a[2][8], b[2][4];    // [set][rows / 16]
-  auto read = [&](int set) {
-    const char* s = lds + get;
+  i32x4 a[2][8], b[2][4];    // [depth half][rows / 16]
+  auto read = [&](int s) {
 #pragma unroll
     for (int n = 0; n < 8; ++n) {
-      a[set][n] = fa.read(s, n);
-      if (n % 2) b[set][n / 2] = fb.read(s + kOperand, n / 2);
+      a[s][n] = fa.read(lds + get_a, n, s);
+      if (n % 2) b[s][n / 2] = fb.read(lds + get_b, n / 2, s);
     }
-    get = get + kStage == kStages * kStage ? 0 : get + kStage;
   };
-  auto multiply = [&](int set) {
+  auto multiply = [&](int s) {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = E::mfma(b[set][j], a[set][i], acc[i][j]);
+      for (int j = 0; j < 4; ++j) acc[i][j] = E::mfma(b[s][j], a[s][i], acc[i][j]);
   };
-  auto turn = [&]() {
+  // What was read has arrived, and all copies but the newest of wide, of every wave.
+  auto turn = [&](auto newer) {
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(wait_counts(4 * (kStages - 2)));
+    __builtin_amdgcn_s_waitcnt(wait_counts(decltype(newer)::value));
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
   };
-  auto spread = [&]() {
+  auto spread = [&](auto copies) {
     constexpr int kReads = (TALL_STRIDED ? 2 : 1) * 8 + (WIDE_STRIDED ? 2 : 1) * 4;
+    constexpr int kCopies = decltype(copies)::value;
 #pragma unroll
-    for (int n = 0; n < kReads; ++n) {
-      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(0x008, kReads > 12 ? 1 : 2, 0);
-    }
-#pragma unroll
-    for (int n = 0; n < 4; ++n) {
+    for (int n = 0; n < kCopies; ++n) {
       __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
       __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
     }
+#pragma unroll
+    for (int n = 0; n < kReads; ++n) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, kReads > 12 ? 1 : kCopies ? 1 : 2, 0);
+    }
   };
 
-  // Step t multiplies from registers while step t + 1 is read from its stage, and step t + 5 copied
-  // to the stage that step t was read from, one turn ago.
-  for (int s = 0; s < kStages; ++s) copy(t0 + s, std::true_type());
-  turn();
+  typedef std::integral_constant<int, 0> C0;
+  typedef std::integral_constant<int, 4> C4;
+  typedef std::integral_constant<int, 8> C8;
+  typedef std::integral_constant<int, 12> C12;
+  copy_a(t0, std::true_type());
+  copy_b(t0, std::true_type());
+  copy_a(t0 + 1, std::true_type());
+  copy_b(t0 + 1, std::true_type());
+  copy_b(t0 + 2, std::true_type());
+  turn(C12());
   read(0);
-  turn();
-  auto pair = [&](int t, auto mask) {
+  auto step = [&](int t, auto mask) {
     read(1);
-    copy(t + kStages, mask);
     multiply(0);
-    spread();
-    turn();
+    spread(C0());
+    turn(C4());              // step t is in registers, step t + 1 in LDS
+    copy_a(t + 2, mask);
+    copy_b(t + 3, mask);
+    get_a = next_a(get_a);
+    get_b = next_b(get_b);
     read(0);
-    copy(t + 1 + kStages, mask);
     multiply(1);
-    spread();
-    turn();
+    spread(C8());
+    __builtin_amdgcn_sched_barrier(0);
   };
   // Steps that no copy has to be masked for: all but a segment's last.
   const int whole = p.depth % kStep == 0 ? t1 : kSegments ? t0 : min(t1, seg_steps - 1);
   int t = t0;
-  for (; t + 1 + kStages < whole; t += 2) pair(t, std::false_type());
-  for (; t < t1; t += 2) pair(t, std::true_type());
+  for (; t + 3 < whole; ++t) step(t, std::false_type());
+  for (; t < t1; ++t) step(t, std::true_type());
   __builtin_amdgcn_s_waitcnt(0);      // the copies past the end land before the sums take their place
   __syncthreads();
 
