@@ -23,6 +23,28 @@ constexpr int kXcds = 8;
 
 constexpr int wait_counts(int vm) { return (vm & 15) | ((vm >> 4) << 14) | (7 << 4); }   // and lgkmcnt(0)
 
+// 16 bytes per lane from src + soff + off to LDS at lds + 16 lane; zeros from `end` bytes behind src on.
+// Through the builtin the compiler waits for every copy in flight before it lets a transposed LDS
+// read pass, since it cannot tell their places apart (depth-contiguous reads it lets pass).  UNSEEN,
+// for the kernels with transposed reads: the same instruction as text, which has no output register
+// to lose (five wait states in front of it: a scalar operand may have been written by a vector
+// instruction); the counted waits of the main loop are what orders copies and reads in either form.
+template <bool UNSEEN>
+__device__ inline void copy_16(char* lds, const char* src, int end, unsigned off, int soff) {
+  if constexpr (UNSEEN) {
+    const uint64_t at = reinterpret_cast<uint64_t>(src);
+    const i32x4 rs = {static_cast<int>(at), static_cast<int>(at >> 32) & 0xFFFF, end, kRsrcWord3};
+    const unsigned to = static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsPtr)lds));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(rs),
+                 "s"(soff)
+                 : "memory");      // m0 has no other use in these kernels
+  } else {
+    const __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), static_cast<short>(0), end, kRsrcWord3);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)lds, 16, off, soff, 0, 0);
+  }
+}
+
 // The copies of a workgroup's 256 rows of an operand, one step after the other: four per wave and
 // step.  Depth-contiguous: the descriptors stay (of two halves for gate and up) and the step is the
 // scalar offset.  Strided: the descriptor moves, and ends with the depth.  Scalars that are compared
@@ -79,7 +101,7 @@ struct Loader {
   }
   // The next step to LDS.  MASK: it may be a segment's last or (unless `read`) behind it: zeros past
   // the depth.  restart: the other segment begins.
-  template <bool MASK, bool SEGMENTS>
+  template <bool MASK, bool SEGMENTS, bool UNSEEN>
   __device__ inline void copy(char* lds, int wave, bool read, bool restart) {
     if (SEGMENTS) {
       src[0] = restart ? second : src[0];
@@ -94,10 +116,7 @@ struct Loader {
       // outputs not stored.
       const int end = STRIDED ? max(min(have, kStep) * row_bytes - skip, 0) : num[h];
       const unsigned o = MASK && !STRIDED && chunk >= have ? kOut : off[j];
-      const __amdgpu_buffer_rsrc_t rs =
-          __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src[h]), static_cast<short>(0), end, kRsrcWord3);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + j * 8192 + wave * 1024), 16, o, STRIDED ? 0 : soff, 0,
-                                               0);
+      copy_16<UNSEEN>(lds + j * 8192 + wave * 1024, src[h], end, o, STRIDED ? 0 : soff);
     }
     if (STRIDED) src[0] += step;
     else soff += kStepBytes;
@@ -179,11 +198,11 @@ __global__ __launch_bounds__(512, 2) void big_kernel(Product p, int splits) {
   auto next_b = [](int at) { return at + kOperand == kEnd ? kWide : at + kOperand; };
   auto restart = [&](int t) { return kSegments && t == seg_steps && t0 < seg_steps; };
   auto copy_a = [&](int t, auto mask) {
-    la.template copy<decltype(mask)::value, kSegments>(lds + put_a, wave, t < t1, restart(t));
+    la.template copy<decltype(mask)::value, kSegments, WIDE_STRIDED>(lds + put_a, wave, t < t1, restart(t));
     put_a = next_a(put_a);
   };
   auto copy_b = [&](int t, auto mask) {
-    lb.template copy<decltype(mask)::value, kSegments>(lds + put_b, wave, t < t1, restart(t));
+    lb.template copy<decltype(mask)::value, kSegments, WIDE_STRIDED>(lds + put_b, wave, t < t1, restart(t));
     put_b = next_b(put_b);
   };
 
