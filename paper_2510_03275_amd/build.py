@@ -25,7 +25,7 @@ ARCH = os.environ.get("SDQ_OFFLOAD_ARCH", "gfx950")
 SOURCES = ["sdq_api.cpp", "encoder.hip", "linear_decode.hip", "linear_prefill.hip", "expand_prefill.hip",
            "prefill_digits.hip",
            "moments.hip", "compensation.hip", "linear_noalloc.hip",
-           "dense_api.cpp", "dense_product.hip", "dense_wide.hip", "dense_big.hip", "dense_few.hip", "dense_quantize.hip"]
+           "dense_api.cpp", "dense_product.hip", "dense_wide.hip", "dense_few.hip", "dense_quantize.hip"]
 
 COMMON = [
     "-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}",
@@ -42,7 +42,6 @@ PER_FILE = {
     "expand_prefill.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "prefill_digits.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     "dense_wide.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-    "dense_big.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
     # the 2-16-row contractions: without it the integer accumulators rotate
     # through AGPR copies, 40 moves per 64-code chunk at 5-8 rows
     "linear_decode.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],

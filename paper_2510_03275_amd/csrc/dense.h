@@ -58,7 +58,6 @@ struct WidePlan {
   int tall = 256, splits = 0;
 };
 WidePlan wide_plan(const Product& p);
-void launch_big(const Product& p, int splits, hipStream_t stream);
 size_t wide_part_bytes(const Product& p, int splits);
 void launch_wide(const Product& p, hipStream_t stream);
 

@@ -210,7 +210,6 @@ static bool rows_aligned(const Product& p) {
 }
 
 size_t product_ws_bytes(const Product& p) {
-  if (p.rows <= 64 && !p.wide_strided) return 0;
   return rows_aligned(p) ? 1 << 28 : 0;
 }
 

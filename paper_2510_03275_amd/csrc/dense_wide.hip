@@ -45,6 +45,7 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "dense_device.h"
 
@@ -55,111 +56,129 @@ typedef __attribute__((address_space(3))) void* LdsPtr;
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4* LdsS4;
 
-constexpr int kWideHalf = 16384;            // bytes of half a tile's rows of wide, one step
-constexpr unsigned kOut = 0x80000000u;      // an offset past every buffer
+constexpr int kStepBytes = 128;                // of depth
+constexpr unsigned kOut = 0x80000000u;         // an offset past every buffer
 constexpr int kRsrcWord3 = 0x00020000;
+constexpr int kXcds = 8;
 
 constexpr int wait_counts(int vm) { return (vm & 15) | ((vm >> 4) << 14) | (7 << 4); }   // and lgkmcnt(0)
 
-__device__ inline void barrier() {
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_sched_barrier(0);
+// 16 bytes per lane from src + soff + off to LDS at lds + 16 lane; zeros from `end` bytes behind src on.
+// Through the builtin the compiler waits for every copy in flight before it lets a transposed LDS
+// read pass, since it cannot tell their places apart (depth-contiguous reads it lets pass).  UNSEEN,
+// for the kernels with transposed reads: the same instruction as text, which has no output register
+// to lose (five wait states in front of it: a scalar operand may have been written by a vector
+// instruction); the counted waits of the main loop are what orders copies and reads in either form.
+template <bool UNSEEN>
+__device__ inline void copy_16(char* lds, const char* src, int end, unsigned off, int soff) {
+  if constexpr (UNSEEN) {
+    const uint64_t at = reinterpret_cast<uint64_t>(src);
+    const i32x4 rs = {static_cast<int>(at), static_cast<int>(at >> 32) & 0xFFFF, end, kRsrcWord3};
+    const unsigned to = static_cast<unsigned>(reinterpret_cast<uintptr_t>((LdsPtr)lds));
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 3\n\tbuffer_load_dwordx4 %1, %2, %3 offen lds" ::"s"(to), "v"(off), "s"(rs),
+                 "s"(soff)
+                 : "memory");      // m0 has no other use in these kernels
+  } else {
+    const __amdgpu_buffer_rsrc_t rs =
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(src), static_cast<short>(0), end, kRsrcWord3);
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)lds, 16, off, soff, 0, 0);
+  }
 }
 
-// The copies of one quarter: half a tile's rows of an operand, one step after the other.
-// Everything but the lane's offsets is the same for the whole wave.
-struct Quarter {
-  const char* src;           // the rows at the next step
-  const char* second;        // the other segment's
-  int64_t bytes, bytes0;     // from there to the operand's end
-  int left;                  // bytes of depth left (depth-contiguous)
-};
+// The copies of a workgroup's ROWS rows of an operand, one step after the other: kCopies per wave and
+// step.  Depth-contiguous: the descriptors stay (of two halves for gate and up) and the step is the
+// scalar offset.  Strided: the descriptor moves, and ends with the depth.  Scalars that are compared
+// are 32 bits wide: no branch splits the loop.
+template <int BYTES, bool STRIDED, bool HALVES, int ROWS>
+struct Loader {
+  static_assert(ROWS == 256 || (!STRIDED && !HALVES), "only whole tiles come strided or in halves");
+  static constexpr int kCopies = ROWS / 64;
+  static constexpr int kStep = kStepBytes / BYTES;
+  const char* src[HALVES ? 2 : 1];
+  int num[HALVES ? 2 : 1];   // depth-contiguous: bytes from src to the last row's end
+  const char* second;        // the other segment
+  int64_t step;              // strided: bytes of a step
+  int soff;                  // depth-contiguous: bytes of the steps done
+  int depth, left;           // of the segment: in bytes (depth-contiguous) or depths
+  int row_bytes, skip;       // strided: of one depth, and in front of the rows
+  unsigned off[kCopies];           // the lane's source offsets
+  int chunk;                 // its place in a step's 128 bytes (depth-contiguous)
 
-// ROWS: of a half.  A wave issues kCopies copies per step and half (of 32 rows, waves 4-7
-// repeat those of waves 0-3).
-template <int BYTES, bool STRIDED, int ROWS>
-struct Copier {
-  static_assert(!STRIDED || ROWS == 128, "strided halves hold 128 rows");
-  static constexpr int kCopies = ROWS == 128 ? 2 : 1;
-  int64_t step;              // bytes from one step to the next
-  int depth_bytes;
-  unsigned off[2];           // the lane's two source offsets
-  int chunk;                 // its 16 bytes of a step (depth-contiguous)
-  __device__ inline void init(int64_t ld, int64_t depth, int wave, int lane) {
+  // Rows r0 .. of n rows, from step t on; steps per segment.
+  __device__ inline void init(const void* first, const void* other, int64_t r0, int64_t n, int64_t ld, int64_t depth_,
+                              int t, int steps, int wave, int lane) {
     const unsigned ld_bytes = static_cast<unsigned>(ld * BYTES);
-    step = STRIDED ? 64 * static_cast<int64_t>(ld_bytes) : 128;
-    depth_bytes = static_cast<int>(depth * BYTES);
-    if (STRIDED) {
-      const int swz = (lane / 16) | ((wave / 2 % 2) << 2);
-      const int r = (((lane % 16) / 2) ^ swz) * 16 + (lane % 2) * 8;
-      off[0] = (4 * wave + lane / 16) * ld_bytes + 2 * r;
-      off[1] = off[0] + 32 * ld_bytes;
-      chunk = 0;
-    } else {
-      chunk = 16 * ((lane % 8) ^ (lane / 8));
-      off[0] = (8 * (ROWS == 32 ? wave % 4 : wave) + lane / 8) * ld_bytes + chunk;
-      off[1] = off[0] + 64 * ld_bytes;
-    }
-  }
-  // Rows r0 .. of n rows (r0 may lie past them: nothing is read then) from step t on; steps per segment.
-  __device__ inline Quarter quarter(const void* first, const void* second, int64_t r0, int64_t n, int64_t ld,
-                                    int64_t depth, int t, int steps) const {
-    Quarter q;
-    const int64_t at = r0 * (STRIDED ? 1 : ld) * BYTES;
-    q.src = static_cast<const char*>(t < steps ? first : second) + at;
-    q.second = static_cast<const char*>(second) + at;
-    // Rows behind a strided operand's last one belong to the next depth: they are read, and
-    // their outputs not stored.
-    const int64_t valid = n - r0;
-    q.bytes0 = STRIDED ? (depth * ld - r0) * BYTES : (valid < ROWS ? valid : ROWS) * ld * BYTES;
-    if (valid <= 0) q.bytes0 = 0;
     const int past = t < steps ? t : t - steps;
-    q.src += past * step;
-    q.bytes = q.bytes0 - past * step;
-    q.left = depth_bytes - 128 * past;
-    return q;
-  }
-  // The next step of q to LDS, zeros unless `read`.
-  __device__ inline void copy(Quarter& q, char* lds, int wave, bool read) const {
-    unsigned o0 = off[0], o1 = off[1];
-    if (!STRIDED) {
-      const bool past = chunk >= q.left;
-      o0 = past ? kOut : o0;
-      o1 = past ? kOut : o1;
+    const int64_t at = r0 * (STRIDED ? 1 : ld) * BYTES;
+    const int valid = static_cast<int>(n) - static_cast<int>(r0);
+    if (STRIDED) {
+      // LDS: [half][64 depths][128 elements]: copy j of wave w holds depths 4 (w + 8 (j % 2)) .. + 3 of half j / 2
+      depth = static_cast<int>(depth_);
+      step = kStep * static_cast<int64_t>(ld_bytes);
+      src[0] = static_cast<const char*>(t < steps ? first : other) + at + past * step;
+      second = static_cast<const char*>(other) + at;
+      row_bytes = static_cast<int>(ld_bytes);
+      skip = static_cast<int>(r0) * BYTES;
+      const int swz = ((lane / 16) << 1) | (wave / 2 % 2);
+      const int r = (((lane % 16) / 2) ^ swz) * 16 + (lane % 2) * 8;
+      for (int j = 0; j < kCopies; ++j) off[j] = (4 * wave + lane / 16 + 32 * (j % 2)) * ld_bytes + 2 * (r + 128 * (j / 2));
+      left = depth - past * kStep;
+      chunk = soff = 0;
+    } else {
+      // LDS: [rows][128 bytes]: copy j of wave w holds rows 8 (w + 8 j) .. + 7
+      depth = static_cast<int>(depth_ * BYTES);
+      src[0] = static_cast<const char*>(t < steps ? first : other) + at;
+      second = static_cast<const char*>(other) + at;
+      num[0] = min(valid, HALVES ? 128 : ROWS) * static_cast<int>(ld_bytes);
+      if (HALVES) {
+        src[HALVES] = second;
+        num[HALVES] = num[0];
+      }
+      chunk = 16 * ((lane % 8) ^ (lane / 8));
+      for (int j = 0; j < kCopies; ++j) off[j] = (8 * wave + lane / 8 + 64 * (HALVES ? j % 2 : j)) * ld_bytes + chunk;
+      soff = past * kStepBytes;
+      left = depth - soff;
+      row_bytes = skip = 0;
     }
-    const int num = !read || q.bytes <= 0 ? 0 : q.bytes < 0x7FFFFFFF ? static_cast<int>(q.bytes) : 0x7FFFFFFF;
-    const __amdgpu_buffer_rsrc_t rs =
-        __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(q.src), static_cast<short>(0), num, kRsrcWord3);
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + (ROWS == 32 ? wave % 4 : wave) * 1024), 16, o0, 0, 0, 0);
-    if (kCopies == 2) __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (LdsPtr)(lds + 8192 + wave * 1024), 16, o1, 0, 0, 0);
-    q.src += step;
-    q.bytes -= step;
-    q.left -= 128;
   }
-  __device__ inline void next_segment(Quarter& q) const {
-    q.src = q.second;
-    q.bytes = q.bytes0;
-    q.left = depth_bytes;
+  // The next step to LDS.  MASK: it may be a segment's last or (unless `read`) behind it: zeros past
+  // the depth.  restart: the other segment begins.
+  template <bool MASK, bool SEGMENTS, bool UNSEEN>
+  __device__ inline void copy(char* lds, int wave, bool read, bool restart) {
+    if (SEGMENTS) {
+      src[0] = restart ? second : src[0];
+      left = restart ? depth : left;
+      soff = restart ? 0 : soff;
+    }
+    const int have = MASK && !read ? 0 : left;
+#pragma unroll
+    for (int j = 0; j < kCopies; ++j) {
+      const int h = HALVES ? j / 2 : 0;
+      // Strided: columns behind the operand's last belong to the next depth: they are read, and their
+      // outputs not stored.
+      const int end = STRIDED ? max(min(have, kStep) * row_bytes - skip, 0) : num[h];
+      const unsigned o = MASK && !STRIDED && chunk >= have ? kOut : off[j];
+      copy_16<UNSEEN>(lds + j * 8192 + wave * 1024, src[h], end, o, STRIDED ? 0 : soff);
+    }
+    if (STRIDED) src[0] += step;
+    else soff += kStepBytes;
+    left -= STRIDED ? kStep : kStepBytes;
   }
 };
 
-// The lane's places in a half for fragments of 16 rows from `row` on.
-template <bool STRIDED>
-struct Places {
-  int at[STRIDED ? 4 : 2];
-  __device__ inline void init(int row, int lane) {
+// The lane's places in an operand's step for a wave's 16 N rows from row0 on.
+template <bool STRIDED, int N>
+struct Frags {
+  int at[STRIDED ? N : 2];
+  __device__ inline void init(int row0, int lane) {
     const int g = lane / 16, i = lane % 16;
     if (STRIDED) {
-      // depth c = 32 s + 8 g + 4 e + i / 4: swizzle i / 4 + 4 (g % 2), the same for every s and e;
-      // row / 16 + n is the granule of fragment n, n ^ handled by the caller's XOR below
-      for (int n = 0; n < 4; ++n) {
-        const int granule = (row / 16 + n) ^ ((i / 4) | ((g % 2) << 2));
-        at[n] = (8 * g + i / 4) * 256 + granule * 32 + (i % 4) * 8;
+      for (int n = 0; n < N; ++n) {
+        const int granule = (row0 % 128 / 16 + n) ^ (((i / 4) << 1) | (g % 2));
+        at[n] = row0 / 128 * 16384 + (8 * g + i / 4) * 256 + granule * 32 + (i % 4) * 8;
       }
     } else {
-      at[0] = (row + i) * 128 + ((g ^ (i % 8)) * 16);
-      at[1] = (row + i) * 128 + (((g + 4) ^ (i % 8)) * 16);
+      for (int s = 0; s < 2; ++s) at[s] = (row0 + i) * kStepBytes + (((4 * s + g) ^ (i % 8)) * 16);
     }
   }
   // Fragment n (16 rows) of depth half s.
@@ -170,35 +189,39 @@ struct Places {
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4)(p + 1024));
       return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      return *reinterpret_cast<const i32x4*>(lds + at[s] + n * 2048);
+      return *reinterpret_cast<const i32x4*>(lds + at[s] + n * 16 * kStepBytes);
     }
   }
 };
 
-constexpr int kXcds = 8;
+// Stages of LDS: as many as 160 KB hold.
+template <int TALL> struct Stages;
+template <> struct Stages<256> { static constexpr int kTall = 2, kWide = 3; };
+template <> struct Stages<128> { static constexpr int kTall = 3, kWide = 3; };
+template <> struct Stages<64> { static constexpr int kTall = 4, kWide = 4; };
 
 template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED, int TALL>
-__global__ __launch_bounds__(512, TALL == 64 ? 4 : 2) void wide_kernel(Product p, int splits) {
+__global__ __launch_bounds__(512, 2) void wide_kernel(Product p, int splits) {
   using E = Elem<ELEM>;
   using Acc = typename E::Acc;
-  constexpr int kB = E::kBytes, kStep = 128 / kB;
-  constexpr int kHalf = TALL / 2, kWaveRows = kHalf / 2, kFrags = kWaveRows / 16;
-  constexpr int kTallHalf = kHalf * 128, kBuf = 2 * kTallHalf + 2 * kWideHalf;
-  using CopyA = Copier<kB, TALL_STRIDED, kHalf>;
-  using CopyB = Copier<kB, WIDE_STRIDED, 128>;
-  __shared__ __attribute__((aligned(1024))) char lds[2 * kBuf];   // [step % 2][A0, A1, B0, B1]
+  constexpr int kB = E::kBytes, kStep = kStepBytes / kB;
+  constexpr int kTallStep = TALL * kStepBytes, kWideStep = 256 * kStepBytes;     // bytes in LDS
+  constexpr int kTallStages = Stages<TALL>::kTall, kWideStages = Stages<TALL>::kWide;
+  constexpr int kWide = kTallStages * kTallStep, kEnd = kWide + kWideStages * kWideStep;
+  constexpr int kFrags = TALL / 32;                 // of 16 rows of tall per wave
+  constexpr int kTallCopies = TALL / 64, kWideCopies = 4;
+  __shared__ __attribute__((aligned(1024))) char lds[kEnd];   // stages of tall, of wide
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int ww = wave % 4, wt = wave / 4;
 
-  // The tile.
   constexpr int kCols = GATED ? 128 : 256;
   const unsigned nw = static_cast<unsigned>((p.cols + kCols - 1) / kCols);
   const unsigned nt = static_cast<unsigned>((p.rows + TALL - 1) / TALL);
   const unsigned total = gridDim.x, id = blockIdx.x;
   const unsigned xcd = id % kXcds, per = total / kXcds, rem = total % kXcds;
   unsigned tile = xcd * per + (xcd < rem ? xcd : rem) + id / kXcds;
-  const int part = __builtin_amdgcn_readfirstlane(tile / (nw * nt));     // of the batch, or of the depth
+  const int part = __builtin_amdgcn_readfirstlane(tile / (nw * nt));
   tile -= part * (nw * nt);
   const int z = splits > 1 ? 0 : part;
   const unsigned band = tile / (4 * nw), in_band = tile - band * (4 * nw);
@@ -211,179 +234,139 @@ __global__ __launch_bounds__(512, TALL == 64 ? 4 : 2) void wide_kernel(Product p
   const int each = steps / splits, more = steps % splits, at = splits > 1 ? part : 0;
   const int t0 = at * each + min(at, more), t1 = t0 + each + (at < more ? 1 : 0);
 
-  CopyA ca;
-  CopyB cb;
-  ca.init(p.ld_tall, p.depth, wave, lane);
-  cb.init(p.ld_wide, p.depth, wave, lane);
-  Quarter qa[2], qb[2];
-#pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    qa[h] = ca.quarter(p.tall[p.batch > 1 ? z : 0], p.tall[1], row0 + kHalf * h, p.rows, p.ld_tall, p.depth, t0,
-                       seg_steps);
-    qb[h] = cb.quarter(p.wide[GATED ? h : 0], p.wide[1], GATED ? col0 : col0 + 128 * h, p.cols, p.ld_wide, p.depth, t0,
-                       seg_steps);
-  }
+  constexpr bool kSegments = WIDE_STRIDED && !TALL_STRIDED;      // two in the gradient of the block's input only
+  Loader<kB, TALL_STRIDED, false, TALL> la;
+  Loader<kB, WIDE_STRIDED, GATED, 256> lb;
+  la.init(p.tall[p.batch > 1 ? z : 0], p.tall[1], row0, p.rows, p.ld_tall, p.depth, t0, seg_steps, wave, lane);
+  lb.init(p.wide[0], p.wide[1], col0, p.cols, p.ld_wide, p.depth, t0, seg_steps, wave, lane);
+  Frags<TALL_STRIDED, kFrags> fa;
+  Frags<WIDE_STRIDED, 4> fb;
+  fa.init(TALL / 2 * wt, lane);
+  fb.init(64 * ww, lane);
 
-  Places<TALL_STRIDED> pa;
-  Places<WIDE_STRIDED> pb;
-  pa.init(kWaveRows * wt, lane);
-  pb.init(32 * ww, lane);
-
-  // Step t of half h to its place: A (tall) or B (wide).
-  auto copy_a = [&](int h, int t) {
-    if (t == seg_steps && t0 < seg_steps && p.segments > 1) ca.next_segment(qa[h]);
-    ca.copy(qa[h], lds + ((t - t0) % 2) * kBuf + h * kTallHalf, wave, t < t1);
+  // LDS offsets of the stages read and filled next.
+  int get_a = 0, get_b = kWide, put_a = 0, put_b = kWide;
+  auto next_a = [](int at) { return at + kTallStep == kWide ? 0 : at + kTallStep; };
+  auto next_b = [](int at) { return at + kWideStep == kEnd ? kWide : at + kWideStep; };
+  auto restart = [&](int t) { return kSegments && t == seg_steps && t0 < seg_steps; };
+  auto copy_a = [&](int t, auto mask) {
+    la.template copy<decltype(mask)::value, kSegments, WIDE_STRIDED>(lds + put_a, wave, t < t1, restart(t));
+    put_a = next_a(put_a);
   };
-  auto copy_b = [&](int h, int t) {
-    if (t == seg_steps && t0 < seg_steps && p.segments > 1) cb.next_segment(qb[h]);
-    cb.copy(qb[h], lds + ((t - t0) % 2) * kBuf + 2 * kTallHalf + h * kWideHalf, wave, t < t1);
+  auto copy_b = [&](int t, auto mask) {
+    lb.template copy<decltype(mask)::value, kSegments, WIDE_STRIDED>(lds + put_b, wave, t < t1, restart(t));
+    put_b = next_b(put_b);
   };
 
-  Acc acc[2][2][kFrags][2] = {};  // [A half][B half][rows of tall / 16][rows of wide / 16]
-  i32x4 a[2][kFrags][2], b[2][2][2];   // halves: [rows / 16][depth half]
-
-#ifndef VAR
-#define VAR 0
-#endif
-#define VPRIO (VAR & 1)
-#define VILV (VAR & 2)
-#define VTWO (VAR & 4)
-  auto multiply = [&](int ha, int hb) {
-    if (!VILV) __builtin_amdgcn_sched_barrier(0);
-    if (VPRIO) __builtin_amdgcn_s_setprio(1);
+  Acc acc[kFrags][4] = {};        // [rows of tall / 16][rows of wide / 16]
+  i32x4 a[2][kFrags], b[2][4];    // [depth half][rows / 16]
+  auto read = [&](int s) {
 #pragma unroll
-    for (int s = 0; s < 2; ++s)
-#pragma unroll
-      for (int i = 0; i < kFrags; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) acc[ha][hb][i][j] = E::mfma(b[hb][j][s], a[ha][i][s], acc[ha][hb][i][j]);
-    if (VPRIO) __builtin_amdgcn_s_setprio(0);
-    if (VILV) {
-#pragma unroll
-      for (int n = 0; n < 8; ++n) {
-        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-        __builtin_amdgcn_sched_group_barrier(0x008, kFrags / 2 ? kFrags / 2 : 1, 0);
-      }
+    for (int n = 0; n < (kFrags > 4 ? kFrags : 4); ++n) {
+      if (n < kFrags) a[s][n] = fa.read(lds + get_a, n, s);
+      if (kFrags <= 4) b[s][n] = fb.read(lds + get_b, n, s);
+      else if (n % 2) b[s][n / 2] = fb.read(lds + get_b, n / 2, s);
     }
-    if (!VTWO) __builtin_amdgcn_sched_barrier(0);
   };
-  auto read_a = [&](const char* buf, int h) {
+  auto multiply = [&](int s) {
 #pragma unroll
     for (int i = 0; i < kFrags; ++i)
 #pragma unroll
-      for (int s = 0; s < 2; ++s) a[h][i][s] = pa.read(buf + h * kTallHalf, i, s);
+      for (int j = 0; j < 4; ++j) acc[i][j] = E::mfma(b[s][j], a[s][i], acc[i][j]);
   };
-  auto read_b = [&](const char* buf, int h) {
-#pragma unroll
-    for (int j = 0; j < 2; ++j)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) b[h][j][s] = pb.read(buf + 2 * kTallHalf + h * kWideHalf, j, s);
-  };
-  // The end of a phase: what was read has arrived, and the quarter read next, of every wave.
-  auto turn = [&]() {
+  // What was read has arrived, and all copies but the newest, of every wave.
+  auto turn = [&](auto newer) {
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(wait_counts(6 + 3 * CopyA::kCopies));   // all but the last six quarters
+    __builtin_amdgcn_s_waitcnt(wait_counts(decltype(newer)::value));
     asm volatile("" ::: "memory");
-    barrier();
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // Copies and LDS reads between the matrix-core instructions.
+  auto spread = [&](auto copies) {
+    constexpr int kReads = (TALL_STRIDED ? 2 : 1) * kFrags + (WIDE_STRIDED ? 2 : 1) * 4;
+    constexpr int kCopies = decltype(copies)::value;
+#pragma unroll
+    for (int n = 0; n < kCopies; ++n) {
+      __builtin_amdgcn_sched_group_barrier(0x020, 1, 0);
+      if (TALL > 64 || n % 2) __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+    }
+#pragma unroll
+    for (int n = 0; n < kReads; ++n) {
+      __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(0x008, TALL == 256 && kReads <= 12 && !kCopies ? 2 : 1, 0);
+    }
   };
 
-  for (int t = t0; t < t0 + 2; ++t) {
-    copy_a(0, t);
-    copy_b(0, t);
-    copy_b(1, t);
-    copy_a(1, t);
+  // Copies newer than a step's, of which the last stages are filled in the order of the steps: where
+  // tall has fewer stages than wide, the newest step of wide.
+  constexpr int kNewer = kTallStages < kWideStages ? kWideCopies : (kTallStages - 2) * (kTallCopies + kWideCopies);
+  typedef std::integral_constant<int, 0> NoCopies;
+  typedef std::integral_constant<int, kTallCopies + kWideCopies> Copies;
+  typedef std::integral_constant<int, kNewer> Newer;
+  typedef std::integral_constant<int, kNewer + kTallCopies + kWideCopies> First;
+#pragma unroll
+  for (int s = 0; s < kWideStages; ++s) {
+    if (s < kTallStages) copy_a(t0 + s, std::true_type());
+    copy_b(t0 + s, std::true_type());
   }
-  turn();
-  read_a(lds, 0);
-  read_b(lds, 0);
-  turn();
-  copy_a(0, t0 + 2);
-  turn();
-
-#if VAR & 4
-  auto turn2 = [&]() {
+  turn(First());
+  read(0);
+  auto step = [&](int t, auto mask) {
+    read(1);
+    multiply(0);
+    spread(NoCopies());
+    turn(Newer());              // step t is in registers, step t + 1 in LDS
+    copy_a(t + kTallStages, mask);
+    copy_b(t + kWideStages, mask);
+    get_a = next_a(get_a);
+    get_b = next_b(get_b);
+    read(0);
+    multiply(1);
+    spread(Copies());
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(wait_counts(4 + 2 * CopyA::kCopies));
-    asm volatile("" ::: "memory");
-    barrier();
   };
-  for (int t = t0; t < t1; ++t) {
-    const char* cur = lds + ((t - t0) % 2) * kBuf;
-    const char* nxt = lds + ((t - t0 + 1) % 2) * kBuf;
-    read_b(cur, 1);
-    copy_b(0, t + 2);
-    multiply(0, 0);
-    read_a(cur, 1);
-    if (t > t0) copy_a(0, t + 2);
-    multiply(0, 1);
-    turn2();
-    read_a(nxt, 0);
-    copy_b(1, t + 2);
-    multiply(1, 0);
-    read_b(nxt, 0);
-    copy_a(1, t + 2);
-    multiply(1, 1);
-    turn2();
-  }
-#else
-  for (int t = t0; t < t1; ++t) {
-    const char* cur = lds + ((t - t0) % 2) * kBuf;
-    const char* nxt = lds + ((t - t0 + 1) % 2) * kBuf;
-    read_b(cur, 1);
-    copy_b(0, t + 2);
-    multiply(0, 0);
-    turn();
-    read_a(cur, 1);
-    copy_b(1, t + 2);
-    multiply(0, 1);
-    turn();
-    read_a(nxt, 0);
-    copy_a(1, t + 2);
-    multiply(1, 0);
-    turn();
-    read_b(nxt, 0);
-    copy_a(0, t + 3);
-    multiply(1, 1);
-    turn();
-  }
-#endif
+  // Steps that no copy has to be masked for: all but a segment's last.
+  const int whole = p.depth % kStep == 0 ? t1 : kSegments ? t0 : min(t1, seg_steps - 1);
+  int t = t0;
+  for (; t + kWideStages < whole; ++t) step(t, std::false_type());
+  for (; t < t1; ++t) step(t, std::true_type());
   __builtin_amdgcn_s_waitcnt(0);      // the copies past the end land before the sums take their place
   __syncthreads();
 
-  // Sums of half a tile: [kHalf rows][64 chunks of four columns], chunk q of row r at q ^ (r % 16).
-  // Chunks 0-31 are of B0, 32-63 of B1.
+  // Sums of (up to) 64 rows of either half of tall: [rows][64 chunks of four columns], chunk q of
+  // row r at q ^ (r % 16).
+  constexpr int kRows = TALL / 2 < 64 ? TALL / 2 : 64, kPasses = TALL / 2 / kRows;
   Acc* sums = reinterpret_cast<Acc*>(lds);
-  const int64_t ld_part = (p.cols + 3) / 4 * 4;      // of gate and of up
+  const int64_t ld_part = (p.cols + 3) / 4 * 4;
 #pragma unroll
-  for (int ha = 0; ha < 2; ++ha) {
-    if (ha) __syncthreads();
+  for (int pass = 0; pass < kPasses; ++pass) {
+    if (pass) __syncthreads();
 #pragma unroll
-    for (int hb = 0; hb < 2; ++hb)
+    for (int i = 0; i < kRows / 16; ++i)
 #pragma unroll
-      for (int i = 0; i < kFrags; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j) {
-          const int r = kWaveRows * wt + 16 * i + lane % 16, q = 32 * hb + 8 * ww + 4 * j + lane / 16;
-          sums[r * 64 + (q ^ (r % 16))] = acc[ha][hb][i][j];
-        }
+      for (int j = 0; j < 4; ++j) {
+        const int r = kRows * wt + 16 * i + lane % 16, q = 16 * ww + 4 * j + lane / 16;
+        sums[r * 64 + (q ^ (r % 16))] = acc[kRows / 16 * pass + i][j];
+      }
     __syncthreads();
     if (splits > 1) {
 #pragma unroll 2
-      for (int o = tid; o < kHalf * 64; o += 512) {
+      for (int o = tid; o < 2 * kRows * 64; o += 512) {
         const int r = o / 64, q = o % 64;
-        const int64_t row = row0 + kHalf * ha + r, c = col0 + 4 * (GATED ? q % 32 : q);
+        const int64_t row = row0 + TALL / 2 * (r / kRows) + kRows * pass + r % kRows, c = col0 + 4 * (GATED ? q % 32 : q);
         if (row >= p.rows || c >= p.cols) continue;
         Acc* dst = static_cast<Acc*>(p.ws) + (part * p.rows + row) * ((GATED ? 2 : 1) * ld_part / 4) +
-                   (GATED ? q / 32 : 0) * (ld_part / 4) + c / 4;
+                    (GATED ? q / 32 : 0) * (ld_part / 4) + c / 4;
         *dst = sums[r * 64 + (q ^ (r % 16))];
       }
       continue;
     }
     constexpr int kOuts = GATED ? 32 : 64;
 #pragma unroll 2
-    for (int o = tid; o < kHalf * kOuts; o += 512) {
+    for (int o = tid; o < 2 * kRows * kOuts; o += 512) {
       const int r = o / kOuts, q = o % kOuts;
-      const int64_t row = row0 + kHalf * ha + r, c = col0 + 4 * q;
+      const int64_t row = row0 + TALL / 2 * (r / kRows) + kRows * pass + r % kRows, c = col0 + 4 * q;
       if (row >= p.rows || c >= p.cols) continue;
       finish4<ELEM, GATED>(p, z, row, c, sums[r * 64 + (q ^ (r % 16))],
                            GATED ? sums[r * 64 + ((q + 32) ^ (r % 16))] : Acc{});
@@ -466,20 +449,8 @@ WidePlan wide_plan(const Product& p) {
 
 void launch_wide(const Product& p, hipStream_t stream) {
   WidePlan plan = wide_plan(p);
-  if (const char* f = getenv("WIDE_FORCE")) sscanf(f, "%d,%d", &plan.tall, &plan.splits);
+  if (const char* f = getenv("WIDE_FORCE")) { sscanf(f, "%d,%d", &plan.tall, &plan.splits); if (p.batch > 1) plan.splits = 1; }
   while (plan.splits > 1 && wide_part_bytes(p, plan.splits) > p.ws_bytes) --plan.splits;
-  if (plan.tall == 256) {
-    launch_big(p, plan.splits, stream);
-    if (plan.splits > 1) {
-      const int64_t quads = (p.cols + 3) / 4 * p.rows;
-      const dim3 grid(static_cast<unsigned>((quads + 255) / 256));
-      if (p.elem == kElemI8 && p.gated) join_kernel<kElemI8, true><<<grid, 256, 0, stream>>>(p, plan.splits);
-      else if (p.elem == kElemI8) join_kernel<kElemI8, false><<<grid, 256, 0, stream>>>(p, plan.splits);
-      else if (p.gated) join_kernel<kElemF16, true><<<grid, 256, 0, stream>>>(p, plan.splits);
-      else join_kernel<kElemF16, false><<<grid, 256, 0, stream>>>(p, plan.splits);
-    }
-    return;
-  }
   if (p.elem == kElemF16) launch_elem<kElemF16>(p, plan, stream);
   else if (p.elem == kElemBf16) launch_elem<kElemBf16>(p, plan, stream);
   else launch_elem<kElemI8>(p, plan, stream);
