@@ -4,6 +4,8 @@
 
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "dense.h"
 
 namespace sdq {
@@ -64,72 +66,79 @@ __device__ inline void act_both(float g, int act, float* value, float* slope) {
   *slope = e > 0.0f && s > 0.0f ? s + g * s * (e * s) * da : s;
 }
 
-__device__ inline float load_as_float(const void* p, int64_t i, int type) {
-  if (type == SDQ_F16) return static_cast<const _Float16*>(p)[i];
-  if (type == SDQ_BF16) return static_cast<const __bf16*>(p)[i];
-  return static_cast<const float*>(p)[i];
-}
-__device__ inline void store_float(void* p, int64_t i, int type, float v) {
-  if (type == SDQ_F16) static_cast<_Float16*>(p)[i] = static_cast<_Float16>(v);
-  else if (type == SDQ_BF16) static_cast<__bf16*>(p)[i] = static_cast<__bf16>(v);
-  else static_cast<float*>(p)[i] = v;
-}
-
-// Four consecutive outputs r .. r + 3 of row i (those below cols); vector
+// Four consecutive outputs r .. r + 3 of row i (those below cols) of type TYPE; vector
 // stores where the row length keeps every group of four aligned.
-__device__ inline void store4(void* out, int64_t i, int64_t r, int64_t cols, int type, bool accumulate, f32x4 v) {
-  const int64_t at = i * cols + r;
-  if (r + 4 <= cols && cols % 4 == 0) {
-    if (type == SDQ_F16) {
-      f16x4* p = reinterpret_cast<f16x4*>(static_cast<_Float16*>(out) + at);
-      if (accumulate) v += __builtin_convertvector(*p, f32x4);
-      *p = __builtin_convertvector(v, f16x4);
-    } else if (type == SDQ_BF16) {
-      bf16x4* p = reinterpret_cast<bf16x4*>(static_cast<__bf16*>(out) + at);
-      if (accumulate) v += __builtin_convertvector(*p, f32x4);
-      *p = __builtin_convertvector(v, bf16x4);
-    } else {
-      f32x4* p = reinterpret_cast<f32x4*>(static_cast<float*>(out) + at);
-      if (accumulate) v += *p;
-      *p = v;
-    }
+template <int TYPE> struct Out;
+template <> struct Out<SDQ_F16> { using Scalar = _Float16; using Four = f16x4; };
+template <> struct Out<SDQ_BF16> { using Scalar = __bf16; using Four = bf16x4; };
+template <> struct Out<SDQ_F32> { using Scalar = float; using Four = f32x4; };
+template <int TYPE>
+__device__ inline void store4(void* out, int64_t i, int64_t r, int64_t cols, bool accumulate, f32x4 v) {
+  using S = typename Out<TYPE>::Scalar;
+  using F = typename Out<TYPE>::Four;
+  S* at = static_cast<S*>(out) + i * cols + r;
+  if (cols % 4 == 0) {
+    F* p = reinterpret_cast<F*>(at);
+    if (accumulate) v += __builtin_convertvector(*p, f32x4);
+    *p = __builtin_convertvector(v, F);
     return;
   }
 #pragma unroll
   for (int j = 0; j < 4; ++j)
-    if (r + j < cols) store_float(out, at + j, type, accumulate ? load_as_float(out, at + j, type) + v[j] : v[j]);
+    if (r + j < cols) at[j] = static_cast<S>(accumulate ? static_cast<float>(at[j]) + v[j] : v[j]);
 }
 
-// The sums of four outputs as floats: 8-bit sums with the scales of their row
-// of tall (st) and of their rows of wide.
-__device__ inline f32x4 scaled4(const f32x4& a, float, const float*, int64_t, int64_t) { return a; }
-__device__ inline f32x4 scaled4(const i32x4& a, float st, const float* sw, int64_t r, int64_t cols) {
-  f32x4 v;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = static_cast<float>(a[j]) * st * sw[min(r + j, cols - 1)];
-  return v;
-}
-
-// Four outputs r .. r + 3 of row i from their sums (GATED: a of gate, b of up).
+// The scales of four rows of wide (of gate and of up), for 8-bit operands.
 template <int ELEM, bool GATED>
+struct WideScales {
+  f32x4 of[GATED ? 2 : 1];
+  __device__ inline void load(const Product& p, int64_t r) {
+    if constexpr (ELEM == kElemI8) {
+#pragma unroll
+      for (int h = 0; h < (GATED ? 2 : 1); ++h)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) of[h][j] = p.wide_scale[h][min(r + j, p.cols - 1)];
+    }
+  }
+};
+
+// Sums as floats: 8-bit ones with the scales of their row of tall and rows of wide.
+template <int ELEM>
+__device__ inline f32x4 as_floats(const typename Elem<ELEM>::Acc& a, float st, const f32x4& sw) {
+  if constexpr (ELEM == kElemI8) return __builtin_convertvector(a, f32x4) * st * sw;
+  else return a;
+}
+
+// Four outputs r .. r + 3 (r < cols) of row i of output z from their sums (GATED: a of gate, b of up).
+template <int ELEM, bool GATED, int TYPE>
 __device__ inline void finish4(const Product& p, int z, int64_t i, int64_t r, const typename Elem<ELEM>::Acc& a,
-                               const typename Elem<ELEM>::Acc& b) {
-  const float st = ELEM == kElemI8 ? p.tall_scale[i] : 1.0f;
-  const f32x4 g = scaled4(a, st, p.wide_scale[0], r, p.cols);
+                               const typename Elem<ELEM>::Acc& b, float st, const WideScales<ELEM, GATED>& sw) {
+  const f32x4 g = as_floats<ELEM>(a, st, sw.of[0]);
   if constexpr (!GATED) {
-    store4(p.out[z], i, r, p.cols, p.out_type, p.accumulate, g);
+    store4<TYPE>(p.out[z], i, r, p.cols, p.accumulate, g);
     return;
   } else {
-    const f32x4 u = scaled4(b, st, p.wide_scale[1], r, p.cols);
+    const f32x4 u = as_floats<ELEM>(b, st, sw.of[GATED]);
     f32x4 h;
 #pragma unroll
     for (int v = 0; v < 4; ++v) h[v] = act_value(g[v], p.act) * u[v];
-    store4(p.out[0], i, r, p.cols, p.out_type, false, h);
-    if (p.g_out) {
-      store4(p.g_out, i, r, p.cols, p.elem, false, g);
-      store4(p.u_out, i, r, p.cols, p.elem, false, u);
+    store4<TYPE>(p.out[0], i, r, p.cols, false, h);
+    if constexpr (ELEM != kElemI8) {
+      if (p.g_out) {      // in the operands' own type, which is h's
+        store4<TYPE>(p.g_out, i, r, p.cols, false, g);
+        store4<TYPE>(p.u_out, i, r, p.cols, false, u);
+      }
     }
   }
+}
+
+// body(the output type as a constant); 16-bit operands have outputs of their own type.
+template <int ELEM, class Body>
+__device__ inline void with_out_type(const Product& p, Body body) {
+  if constexpr (ELEM != kElemI8) body(std::integral_constant<int, ELEM>());
+  else if (p.out_type == SDQ_F16) body(std::integral_constant<int, SDQ_F16>());
+  else if (p.out_type == SDQ_BF16) body(std::integral_constant<int, SDQ_BF16>());
+  else body(std::integral_constant<int, SDQ_F32>());
 }
 
 }  // namespace sdq

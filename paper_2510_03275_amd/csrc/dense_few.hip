@@ -118,7 +118,13 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Product p) {
     const int t = o % kColTiles, j = o / kColTiles;
     const int64_t row = 16 * j + lane % 16, r = col0 + 16 * t + 4 * (lane / 16);
     if (row >= p.rows || r >= p.cols) continue;
-    finish4<ELEM, GATED>(p, 0, row, r, part[0][t][j][lane], part[0][GATED ? kColTiles + t : t][j][lane]);
+    WideScales<ELEM, GATED> sw;
+    sw.load(p, r);
+    with_out_type<ELEM>(p, [&](auto type) {
+      finish4<ELEM, GATED, decltype(type)::value>(p, 0, row, r, part[0][t][j][lane],
+                                                  part[0][GATED ? kColTiles + t : t][j][lane],
+                                                  ELEM == kElemI8 ? p.tall_scale[row] : 1.0f, sw);
+    });
   }
 }
 

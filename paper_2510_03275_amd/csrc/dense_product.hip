@@ -118,26 +118,15 @@ __global__ __launch_bounds__(256) void product_kernel(Product p) {
     const int64_t i = row0 + 32 * wt + 16 * j + lane % 16;
     if (i >= p.rows) continue;
     const float st = ELEM == kElemI8 ? p.tall_scale[i] : 1.0f;
-    if (GATED) {
-      const int64_t r = col0 + 16 * wr + 4 * (lane / 16);
+#pragma unroll
+    for (int w = 0; w < (GATED ? 1 : 2); ++w) {
+      const int64_t r = col0 + (GATED ? 16 : 32) * wr + 16 * w + 4 * (lane / 16);
       if (r >= p.cols) continue;
-      const f32x4 g = scaled4(acc[0][j], st, p.wide_scale[0], r, p.cols);
-      const f32x4 u = scaled4(acc[1][j], st, p.wide_scale[1], r, p.cols);
-      f32x4 h;
-#pragma unroll
-      for (int v = 0; v < 4; ++v) h[v] = act_value(g[v], p.act) * u[v];
-      store4(p.out[0], i, r, p.cols, p.out_type, false, h);
-      if (p.g_out) {
-        store4(p.g_out, i, r, p.cols, p.elem, false, g);
-        store4(p.u_out, i, r, p.cols, p.elem, false, u);
-      }
-    } else {
-#pragma unroll
-      for (int w = 0; w < 2; ++w) {
-        const int64_t r = col0 + 32 * wr + 16 * w + 4 * (lane / 16);
-        if (r >= p.cols) continue;
-        store4(p.out[z], i, r, p.cols, p.out_type, p.accumulate, scaled4(acc[w][j], st, p.wide_scale[0], r, p.cols));
-      }
+      WideScales<ELEM, GATED> sw;
+      sw.load(p, r);
+      with_out_type<ELEM>(p, [&](auto type) {
+        finish4<ELEM, GATED, decltype(type)::value>(p, z, i, r, acc[w][j], acc[1][j], st, sw);
+      });
     }
   }
 }

@@ -338,7 +338,16 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p, int splits) {
   // row r at q ^ (r % 16).
   constexpr int kRows = TALL / 2 < 64 ? TALL / 2 : 64, kPasses = TALL / 2 / kRows;
   Acc* sums = reinterpret_cast<Acc*>(lds);
-  const int64_t ld_part = (p.cols + 3) / 4 * 4;
+  float* row_scales = reinterpret_cast<float*>(lds + 2 * kRows * 1024);      // of the tile's rows of tall
+  static_assert(2 * kRows * 1024 + TALL * 4 <= kEnd, "the sums and scales fit");
+  if (ELEM == kElemI8 && tid < TALL) row_scales[tid] = p.tall_scale[min(row0 + tid, p.rows - 1)];
+  const int64_t ld_part = (p.cols + 3) / 4 * 4;      // of gate and of up
+  constexpr int kOuts = GATED ? 32 : 64, kTurns = 2 * kRows * kOuts / 512;
+  // A thread's outputs lie in one chunk of columns.
+  const int q = tid % kOuts;
+  const int64_t c = col0 + 4 * q;
+  WideScales<ELEM, GATED> wide_scales;
+  if (splits == 1) wide_scales.load(p, c);
 #pragma unroll
   for (int pass = 0; pass < kPasses; ++pass) {
     if (pass) __syncthreads();
@@ -346,31 +355,30 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p, int splits) {
     for (int i = 0; i < kRows / 16; ++i)
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        const int r = kRows * wt + 16 * i + lane % 16, q = 16 * ww + 4 * j + lane / 16;
-        sums[r * 64 + (q ^ (r % 16))] = acc[kRows / 16 * pass + i][j];
+        const int r = kRows * wt + 16 * i + lane % 16, at = 16 * ww + 4 * j + lane / 16;
+        sums[r * 64 + (at ^ (r % 16))] = acc[kRows / 16 * pass + i][j];
       }
     __syncthreads();
-    if (splits > 1) {
-#pragma unroll 2
-      for (int o = tid; o < 2 * kRows * 64; o += 512) {
-        const int r = o / 64, q = o % 64;
-        const int64_t row = row0 + TALL / 2 * (r / kRows) + kRows * pass + r % kRows, c = col0 + 4 * (GATED ? q % 32 : q);
-        if (row >= p.rows || c >= p.cols) continue;
-        Acc* dst = static_cast<Acc*>(p.ws) + (part * p.rows + row) * ((GATED ? 2 : 1) * ld_part / 4) +
-                    (GATED ? q / 32 : 0) * (ld_part / 4) + c / 4;
-        *dst = sums[r * 64 + (q ^ (r % 16))];
+    if (c >= p.cols) continue;
+    auto outputs = [&](auto type) {
+#pragma unroll 4
+      for (int n = 0; n < kTurns; ++n) {
+        const int r = tid / kOuts + n * (512 / kOuts), tile_row = TALL / 2 * (r / kRows) + kRows * pass + r % kRows;
+        const int64_t row = row0 + tile_row;
+        const Acc a = sums[r * 64 + (q ^ (r % 16))], b = GATED ? sums[r * 64 + ((q + 32) ^ (r % 16))] : Acc{};
+        if (row >= p.rows) continue;
+        if constexpr (decltype(type)::value < 0) {
+          Acc* dst = static_cast<Acc*>(p.ws) + (part * p.rows + row) * ((GATED ? 2 : 1) * ld_part / 4) + c / 4;
+          dst[0] = a;
+          if (GATED) dst[ld_part / 4] = b;
+        } else {
+          finish4<ELEM, GATED, decltype(type)::value>(p, z, row, c, a, b, ELEM == kElemI8 ? row_scales[tile_row] : 1.0f,
+                                                      wide_scales);
+        }
       }
-      continue;
-    }
-    constexpr int kOuts = GATED ? 32 : 64;
-#pragma unroll 2
-    for (int o = tid; o < 2 * kRows * kOuts; o += 512) {
-      const int r = o / kOuts, q = o % kOuts;
-      const int64_t row = row0 + TALL / 2 * (r / kRows) + kRows * pass + r % kRows, c = col0 + 4 * q;
-      if (row >= p.rows || c >= p.cols) continue;
-      finish4<ELEM, GATED>(p, z, row, c, sums[r * 64 + (q ^ (r % 16))],
-                           GATED ? sums[r * 64 + ((q + 32) ^ (r % 16))] : Acc{});
-    }
+    };
+    if (splits > 1) outputs(std::integral_constant<int, -1>());
+    else with_out_type<ELEM>(p, outputs);
   }
 }
 
@@ -387,7 +395,11 @@ __global__ __launch_bounds__(256) void join_kernel(Product p, int splits) {
     a += src[s * p.rows * ld];
     if (GATED) b += src[s * p.rows * ld + quads];
   }
-  finish4<ELEM, GATED>(p, 0, row, 4 * q, a, b);
+  WideScales<ELEM, GATED> sw;
+  sw.load(p, 4 * q);
+  with_out_type<ELEM>(p, [&](auto type) {
+    finish4<ELEM, GATED, decltype(type)::value>(p, 0, row, 4 * q, a, b, ELEM == kElemI8 ? p.tall_scale[row] : 1.0f, sw);
+  });
 }
 
 template <int ELEM, bool WS, bool TS, bool GATED, int TALL>
