@@ -40,32 +40,37 @@ struct Product {
   int act = SDQ_ACT_SILU;
   void* g_out = nullptr;   // gated: the projections themselves (16-bit, type elem), or NULL
   void* u_out = nullptr;
-  // partial sums of products split over depth, ws_bytes of them
+  // product_ws_bytes of workspace
   void* ws = nullptr;
-  size_t ws_bytes = 0;
 };
 
-// The workspace launch_product makes use of for this product (ws and ws_bytes not read).
+// The workspace that launch_product needs for this product (pointers not read): copies of
+// operands whose rows do not start 16-byte aligned, partial sums.
 size_t product_ws_bytes(const Product& p);
+// The elements from row to row with which the product takes an operand of n-element rows as it
+// is; elements past n are then zeros (depth-contiguous) or anything (strided).
+int64_t product_ld(const Product& p, int64_t n);
 sdq_status launch_product(const Product& p, hipStream_t stream);
 
-// At most 64 rows, neither operand strided.
+// The kernels behind it.  At most 64 rows, neither operand strided, rows at any alignment
+// (dense_few.hip):
 void launch_few(const Product& p, hipStream_t stream);
-// The product on tiles of 256 rows of wide (dense_wide.hip), rows aligned as launch_product
-// checks it: how many rows of tall to a tile, and into how many parts the depth is cut, whose
-// sums take wide_part_bytes of the workspace.
+// Tiles of 256 rows of wide, rows aligned (dense_wide.hip): how many rows of tall to a tile, and into
+// how many parts the depth is cut, whose sums take wide_part_bytes of the workspace.
 struct WidePlan {
   int tall = 256, splits = 0;
 };
 WidePlan wide_plan(const Product& p);
 size_t wide_part_bytes(const Product& p, int splits);
-void launch_wide(const Product& p, hipStream_t stream);
+void launch_wide(const Product& p, const WidePlan& plan, hipStream_t stream);
 
-sdq_status launch_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, int8_t* q, float* scales,
-                                hipStream_t stream);
+// Codes in rows of ld, those past k zeros.
+sdq_status launch_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, int8_t* q, int64_t ld,
+                                float* scales, hipStream_t stream);
 
-// dg = dh u act'(g) and du = dh act(g), rounded to the type t of every operand.
-sdq_status launch_gate_gradient(const void* dh, const void* g, const void* u, sdq_dtype t, int64_t count, int act,
-                                void* dg, void* du, hipStream_t stream);
+// dg = dh u act'(g) and du = dh act(g), [m x f], rounded to the type t of every operand; dg and du in
+// rows of ld (a multiple of 8), zeros past f.
+sdq_status launch_gate_gradient(const void* dh, const void* g, const void* u, sdq_dtype t, int64_t m, int64_t f,
+                                int64_t ld, int act, void* dg, void* du, hipStream_t stream);
 
 }  // namespace sdq

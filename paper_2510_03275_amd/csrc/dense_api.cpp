@@ -13,7 +13,8 @@ bool float_type(sdq_dtype t) { return t == SDQ_F16 || t == SDQ_BF16 || t == SDQ_
 bool half_type(sdq_dtype t) { return t == SDQ_F16 || t == SDQ_BF16; }
 bool known_act(int32_t act) { return act == SDQ_ACT_SILU || act == SDQ_ACT_GELU_TANH; }
 
-constexpr int64_t kMaxSize = int64_t{1} << 30;    // rows, cols and depth
+constexpr int64_t kMaxRows = int64_t{1} << 29;
+constexpr int64_t kMaxRowLength = (int64_t{1} << 22) - 16;   // 256 rows of 16-bit elements are addressed with 31 bits
 constexpr int64_t kMaxInt8Depth = 131071;         // 128 * 128 * k stays below 2^31
 constexpr int64_t kMaxTiles = int64_t{1} << 23;   // of 32 x 64 outputs: threads of one launch fit 32 bits
 
@@ -24,7 +25,7 @@ sdq_status check_sizes(int64_t m, int64_t n, int64_t k, bool int8) {
   if (int8 && k > kMaxInt8Depth)
     return set_error(SDQ_ERR_SHAPE, "k=%lld: 8-bit sums are exact in 32 bits up to k = %lld", (long long)k,
                      (long long)kMaxInt8Depth);
-  if (m > kMaxSize || n > kMaxSize || k > kMaxSize || ((m + 63) / 64) * ((n + 31) / 32) > kMaxTiles ||
+  if (m > kMaxRows || n > kMaxRowLength || k > kMaxRowLength || ((m + 63) / 64) * ((n + 31) / 32) > kMaxTiles ||
       ((n + 63) / 64) * ((k + 31) / 32) > kMaxTiles || ((m + 63) / 64) * ((k + 31) / 32) > kMaxTiles)
     return set_error(SDQ_ERR_SHAPE, "m=%lld n=%lld k=%lld is too large for one launch", (long long)m, (long long)n,
                      (long long)k);
@@ -64,15 +65,16 @@ struct Int8Space {
   int8_t* q;
   float* scales;
   void* product;
-  size_t product_bytes, bytes;
+  size_t bytes;
 };
+// Codes and scales of x (rows as the product takes them), then the product's own workspace, which is
+// larger for codes given with rows that do not start aligned.
 Int8Space int8_space(const Product& p, void* ws) {
   Int8Space s;
   Carver c{static_cast<char*>(ws)};
-  s.q = static_cast<int8_t*>(c.take(static_cast<size_t>(p.rows) * p.depth));
+  s.q = static_cast<int8_t*>(c.take(static_cast<size_t>(p.rows) * product_ld(p, p.depth)));
   s.scales = static_cast<float*>(c.take(static_cast<size_t>(p.rows) * 4));
-  s.product_bytes = product_ws_bytes(p);
-  s.product = c.take(s.product_bytes);
+  s.product = c.take(product_ws_bytes(p));
   s.bytes = c.off;
   return s;
 }
@@ -92,13 +94,14 @@ sdq_status run_int8(Product p, const void* x, sdq_dtype xt, const float* x_scale
     p.tall[0] = x;
     p.tall_scale = x_scales;
   } else {
-    st = launch_int8_quantize(x, xt, p.rows, p.depth, s.q, s.scales, stream);
+    const int64_t ld = product_ld(p, p.depth);
+    st = launch_int8_quantize(x, xt, p.rows, p.depth, s.q, ld, s.scales, stream);
     if (st != SDQ_OK) return st;
     p.tall[0] = s.q;
+    p.ld_tall = ld;
     p.tall_scale = s.scales;
   }
   p.ws = s.product;
-  p.ws_bytes = s.product_bytes;
   return launch_product(p, stream);
 }
 
@@ -121,10 +124,10 @@ Product input_gradient(sdq_dtype t, int64_t m, int64_t f, int64_t k) {
   p.cols = k;
   p.depth = f;
   p.ld_wide = k;
-  p.ld_tall = f;
   p.wide_strided = true;
   p.segments = 2;
   p.out_type = t;
+  p.ld_tall = product_ld(p, f);
   return p;
 }
 
@@ -136,26 +139,28 @@ Product weight_gradient(sdq_dtype t, int64_t m, int64_t f, int64_t k) {
   p.cols = k;
   p.depth = m;
   p.ld_wide = k;
-  p.ld_tall = f;
   p.wide_strided = p.tall_strided = true;
   p.batch = 2;
   p.out_type = t;
+  p.ld_tall = product_ld(p, f);
   return p;
 }
 
 struct BackwardSpace {
   void *dg, *du, *product;
-  size_t product_bytes, bytes;
+  int64_t ld;      // of dg and du
+  size_t bytes;
 };
 BackwardSpace backward_space(sdq_dtype t, int64_t m, int64_t f, int64_t k, void* ws) {
   BackwardSpace s;
   Carver c{static_cast<char*>(ws)};
-  const size_t bytes = static_cast<size_t>(m) * f * 2;
+  const Product x = input_gradient(t, m, f, k), w = weight_gradient(t, m, f, k);
+  s.ld = x.ld_tall;
+  const size_t bytes = static_cast<size_t>(m) * s.ld * 2;
   s.dg = c.take(bytes);
   s.du = c.take(bytes);
-  const size_t a = product_ws_bytes(input_gradient(t, m, f, k)), b = product_ws_bytes(weight_gradient(t, m, f, k));
-  s.product_bytes = a > b ? a : b;
-  s.product = c.take(s.product_bytes);
+  const size_t a = product_ws_bytes(x), b = product_ws_bytes(w);
+  s.product = c.take(a > b ? a : b);
   s.bytes = c.off;
   return s;
 }
@@ -168,12 +173,12 @@ sdq_status sdq_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, 
                              void* stream) {
   if (!float_type(xt)) return set_error(SDQ_ERR_ARG, "bad dtype");
   if (m < 0 || k <= 0) return set_error(SDQ_ERR_ARG, "need m >= 0 and k > 0");
-  if (m > kMaxTiles || k > kMaxSize) return set_error(SDQ_ERR_SHAPE, "m=%lld k=%lld is too large for one launch",
+  if (m > kMaxTiles || k > kMaxRows) return set_error(SDQ_ERR_SHAPE, "m=%lld k=%lld is too large for one launch",
                                                       (long long)m, (long long)k);
   if (m == 0) return SDQ_OK;
   if (!x || !q || !scales) return set_error(SDQ_ERR_ARG, "NULL pointer argument");
   if (!aligned16(x) || !aligned16(q)) return set_error(SDQ_ERR_ARG, "x and q must be 16-byte aligned");
-  return launch_int8_quantize(x, xt, m, k, q, scales, static_cast<hipStream_t>(stream));
+  return launch_int8_quantize(x, xt, m, k, q, k, scales, static_cast<hipStream_t>(stream));
 }
 
 size_t sdq_int8_linear_workspace_bytes(int64_t m, int64_t n, int64_t k) { return int8_bytes(m, n, k, false); }
@@ -239,8 +244,7 @@ sdq_status sdq_gated_linear(const void* x, sdq_dtype t, int64_t m, const void* g
     return set_error(SDQ_ERR_ARG, "x, gate, up, h, g and u must be 16-byte aligned");
   Product p = gated_product(t, m, f, k);
   p.ws = ws;
-  p.ws_bytes = product_ws_bytes(p);
-  st = check_workspace(p.ws_bytes, ws, ws_bytes);
+  st = check_workspace(product_ws_bytes(p), ws, ws_bytes);
   if (st != SDQ_OK) return st;
   p.tall[0] = x;
   p.wide[0] = gate;
@@ -279,7 +283,7 @@ sdq_status sdq_gated_linear_backward(const void* dh, const void* x, sdq_dtype t,
   const hipStream_t hs = static_cast<hipStream_t>(stream);
   if (!dx && !dgate) return SDQ_OK;
   if (m > 0 && f > 0) {
-    st = launch_gate_gradient(dh, g, u, t, m * f, act, s.dg, s.du, hs);
+    st = launch_gate_gradient(dh, g, u, t, m, f, s.ld, act, s.dg, s.du, hs);
     if (st != SDQ_OK) return st;
   }
   // Without rows or features the sums are empty: the products write zeros.
@@ -291,7 +295,6 @@ sdq_status sdq_gated_linear_backward(const void* dh, const void* x, sdq_dtype t,
     p.tall[1] = s.du;
     p.out[0] = dx;
     p.ws = s.product;
-    p.ws_bytes = s.product_bytes;
     st = launch_product(p, hs);
     if (st != SDQ_OK) return st;
   }
@@ -304,7 +307,6 @@ sdq_status sdq_gated_linear_backward(const void* dh, const void* x, sdq_dtype t,
     p.out[1] = dup;
     p.accumulate = accumulate != 0;
     p.ws = s.product;
-    p.ws_bytes = s.product_bytes;
     st = launch_product(p, hs);
   }
   return st;

@@ -29,13 +29,13 @@ __device__ inline int quantized(float x, float s, float inv) {
 
 template <class S>
 __global__ __launch_bounds__(256) void quantize_rows_kernel(const S* __restrict__ x, int64_t k, int8_t* __restrict__ q,
-                                                            float* __restrict__ scales) {
+                                                            int64_t ld, float* __restrict__ scales) {
   constexpr int kPer = 16 / sizeof(S);
   __shared__ float part[4];
   const int64_t row = blockIdx.x;
   const int tid = threadIdx.x;
   const S* src = x + row * k;
-  int8_t* dst = q + row * k;
+  int8_t* dst = q + row * ld;
   const int64_t whole = k / kPer * kPer;
   float a = 0.0f;
   for (int64_t c = tid * kPer; c < whole; c += 256 * kPer) {
@@ -65,19 +65,20 @@ __global__ __launch_bounds__(256) void quantize_rows_kernel(const S* __restrict_
   }
   if (whole + tid < k)
     dst[whole + tid] = finite ? static_cast<int8_t>(quantized(static_cast<float>(src[whole + tid]), s, inv)) : 0;
+  if (k + tid < ld) dst[k + tid] = 0;      // ld - k < 16
 }
 
 }  // namespace
 
-sdq_status launch_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, int8_t* q, float* scales,
-                                hipStream_t stream) {
+sdq_status launch_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, int8_t* q, int64_t ld,
+                                float* scales, hipStream_t stream) {
   const dim3 grid(static_cast<unsigned>(m));
   if (xt == SDQ_F16)
-    quantize_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<const _Float16*>(x), k, q, scales);
+    quantize_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<const _Float16*>(x), k, q, ld, scales);
   else if (xt == SDQ_BF16)
-    quantize_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<const __bf16*>(x), k, q, scales);
+    quantize_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<const __bf16*>(x), k, q, ld, scales);
   else
-    quantize_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<const float*>(x), k, q, scales);
+    quantize_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<const float*>(x), k, q, ld, scales);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SDQ_OK : hip_error(e, "int8 quantize launch");
 }

@@ -91,7 +91,7 @@ __device__ inline void copy_16(char* lds, const char* src, int end, unsigned off
 // are 32 bits wide: no branch splits the loop.
 template <int BYTES, bool STRIDED, bool HALVES, int ROWS>
 struct Loader {
-  static_assert(ROWS == 256 || (!STRIDED && !HALVES), "only whole tiles come strided or in halves");
+  static_assert(ROWS == 256 || (!HALVES && !(STRIDED && ROWS == 64)), "halves of 128 rows");
   static constexpr int kCopies = ROWS / 64;
   static constexpr int kStep = kStepBytes / BYTES;
   const char* src[HALVES ? 2 : 1];
@@ -223,7 +223,7 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p, int splits) {
   unsigned tile = xcd * per + (xcd < rem ? xcd : rem) + id / kXcds;
   const int part = __builtin_amdgcn_readfirstlane(tile / (nw * nt));
   tile -= part * (nw * nt);
-  const int z = splits > 1 ? 0 : part;
+  const int z = p.batch > 1 ? part % p.batch : 0, at = p.batch > 1 ? part / p.batch : part;   // output, part of the depth
   const unsigned band = tile / (4 * nw), in_band = tile - band * (4 * nw);
   const unsigned band_rows = nt - 4 * band < 4 ? nt - 4 * band : 4;
   const unsigned tw = in_band / band_rows, tt = 4 * band + (in_band - tw * band_rows);
@@ -231,7 +231,7 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p, int splits) {
   const int64_t col0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(tw)) * kCols;
 
   const int seg_steps = static_cast<int>((p.depth + kStep - 1) / kStep), steps = seg_steps * p.segments;
-  const int each = steps / splits, more = steps % splits, at = splits > 1 ? part : 0;
+  const int each = steps / splits, more = steps % splits;
   const int t0 = at * each + min(at, more), t1 = t0 + each + (at < more ? 1 : 0);
 
   constexpr bool kSegments = WIDE_STRIDED && !TALL_STRIDED;      // two in the gradient of the block's input only
@@ -387,18 +387,21 @@ template <int ELEM, bool GATED>
 __global__ __launch_bounds__(256) void join_kernel(Product p, int splits) {
   using Acc = typename Elem<ELEM>::Acc;
   const int64_t quads = (p.cols + 3) / 4, o = blockIdx.x * int64_t{256} + threadIdx.x;
-  if (o >= quads * p.rows) return;
-  const int64_t row = o / quads, q = o - row * quads, ld = (GATED ? 2 : 1) * quads;
-  const Acc* src = static_cast<const Acc*>(p.ws) + row * ld + q;
+  if (o >= quads * p.rows * p.batch) return;
+  const int64_t line = o / quads, q = o - line * quads, ld = (GATED ? 2 : 1) * quads;      // rows of every output
+  const int z = static_cast<int>(line / p.rows);
+  const int64_t row = line - z * p.rows, stride = p.batch * p.rows * ld;
+  const Acc* src = static_cast<const Acc*>(p.ws) + line * ld + q;
   Acc a = {}, b = {};
+#pragma unroll 4
   for (int s = 0; s < splits; ++s) {
-    a += src[s * p.rows * ld];
-    if (GATED) b += src[s * p.rows * ld + quads];
+    a += src[s * stride];
+    if (GATED) b += src[s * stride + quads];
   }
   WideScales<ELEM, GATED> sw;
   sw.load(p, 4 * q);
   with_out_type<ELEM>(p, [&](auto type) {
-    finish4<ELEM, GATED, decltype(type)::value>(p, 0, row, 4 * q, a, b, ELEM == kElemI8 ? p.tall_scale[row] : 1.0f, sw);
+    finish4<ELEM, GATED, decltype(type)::value>(p, z, row, 4 * q, a, b, ELEM == kElemI8 ? p.tall_scale[row] : 1.0f, sw);
   });
 }
 
@@ -409,7 +412,7 @@ void launch_tiles(const Product& p, int splits, hipStream_t stream) {
   wide_kernel<ELEM, WS, TS, GATED, TALL>
       <<<dim3(static_cast<unsigned>(tiles * p.batch * splits)), 512, 0, stream>>>(p, splits);
   if (splits > 1) {
-    const int64_t quads = (p.cols + 3) / 4 * p.rows;
+    const int64_t quads = (p.cols + 3) / 4 * p.rows * p.batch;
     join_kernel<ELEM, GATED><<<dim3(static_cast<unsigned>((quads + 255) / 256)), 256, 0, stream>>>(p, splits);
   }
 }
@@ -425,6 +428,7 @@ template <int ELEM>
 void launch_elem(const Product& p, const WidePlan& plan, hipStream_t stream) {
   if (p.gated) return launch_tall<ELEM, false, true>(p, plan, stream);
   if constexpr (ELEM == kElemI8) launch_tall<ELEM, false, false>(p, plan, stream);
+  else if (p.tall_strided && plan.tall == 128) launch_tiles<ELEM, true, true, false, 128>(p, plan.splits, stream);
   else if (p.tall_strided) launch_tiles<ELEM, true, true, false, 256>(p, plan.splits, stream);
   else launch_tall<ELEM, true, false>(p, plan, stream);
 }
@@ -432,23 +436,31 @@ void launch_elem(const Product& p, const WidePlan& plan, hipStream_t stream) {
 }  // namespace
 
 size_t wide_part_bytes(const Product& p, int splits) {
-  return splits > 1 ? static_cast<size_t>(p.rows) * ((p.cols + 3) / 4) * 16 * (p.gated ? 2 : 1) * splits : 0;
+  return splits > 1 ? static_cast<size_t>(p.batch) * p.rows * ((p.cols + 3) / 4) * 16 * (p.gated ? 2 : 1) * splits : 0;
 }
 
+// The plan with the least time by a model fitted to measured ones (8-bit and bf16 products of 8 to
+// 900 rows with 768 x 768 to 28672 x 8192 weights, every tile height and 1 to 16 splits; it picks one
+// within 10 % of the fastest of them but for single cases):
+//   a launch 2.5 us; a turn of the chip 2, 3.5 or 7.5 us for its first copies and its outputs and
+//   0.62, 0.72 or 1.1 us per step at 64, 128 or 256 rows of tall, up to 45 % more with every compute
+//   unit at work (power), or what the turn's rows of wide take from memory at 5.5 TB/s;
+//   the partial sums 2.5 us and their bytes, written and read, at 6 TB/s.
 WidePlan wide_plan(const Product& p) {
-  const int64_t bytes = p.elem == kElemI8 ? 1 : 2;
-  const int64_t steps = (p.depth * bytes + 127) / 128 * p.segments, units = device_compute_units();
-  const int64_t col_tiles = (p.cols + (p.gated ? 127 : 255)) / (p.gated ? 128 : 256);
+  const int64_t bytes = p.elem == kElemI8 ? 1 : 2, units = device_compute_units();
+  const int64_t steps = (p.depth * bytes + 127) / 128 * p.segments;
+  const int64_t col_tiles = (p.cols + (p.gated ? 127 : 255)) / (p.gated ? 128 : 256) * p.batch;
   WidePlan best;
   double best_us = 0;
-  for (int tall = 256; tall >= (p.tall_strided ? 256 : 64); tall /= 2) {
-    const int64_t tiles = col_tiles * ((p.rows + tall - 1) / tall) * p.batch;
-    const int64_t at_once = tall == 64 ? 2 * units : units;
-    const double step_us = tall == 256 ? 0.95 : tall == 128 ? 0.6 : 0.9, fixed_us = tall == 256 ? 6 : 4;
-    for (int splits = 1; splits <= (p.batch > 1 ? 1 : 32) && (splits == 1 || steps / splits >= 4); ++splits) {
-      const int64_t turns = (tiles * splits + at_once - 1) / at_once;
-      const double us = turns * (fixed_us + ((steps + splits - 1) / splits) * step_us) +
-                        (splits > 1 ? 3.0 + wide_part_bytes(p, splits) * 2e-6 / 4.0 : 0.0);
+  for (int tall = 256; tall >= (p.tall_strided ? 128 : 64); tall /= 2) {
+    const int64_t tiles = col_tiles * ((p.rows + tall - 1) / tall);
+    const double step = tall == 256 ? 1.1 : tall == 128 ? 0.72 : 0.62, ends = tall == 256 ? 7.5 : tall == 128 ? 3.5 : 2.0;
+    for (int splits = 1; splits <= 32 && (splits == 1 || steps / splits >= 3); ++splits) {
+      const int64_t at_once = std::min(tiles * splits, units), turns = (tiles * splits + units - 1) / units;
+      const double busy = static_cast<double>(at_once) / units;
+      const double memory = std::min(col_tiles * splits, at_once) * 32768.0 / 5.5e6;
+      double us = 2.5 + turns * (ends + (steps + splits - 1) / splits * std::max(step * (1 + 0.45 * busy), memory));
+      if (splits > 1) us += 2.5 + wide_part_bytes(p, splits) * 2 / 6e6;
       if (best.splits == 0 || us < best_us) {
         best.tall = tall;
         best.splits = splits;
@@ -459,10 +471,7 @@ WidePlan wide_plan(const Product& p) {
   return best;
 }
 
-void launch_wide(const Product& p, hipStream_t stream) {
-  WidePlan plan = wide_plan(p);
-  if (const char* f = getenv("WIDE_FORCE")) { sscanf(f, "%d,%d", &plan.tall, &plan.splits); if (p.batch > 1) plan.splits = 1; }
-  while (plan.splits > 1 && wide_part_bytes(p, plan.splits) > p.ws_bytes) --plan.splits;
+void launch_wide(const Product& p, const WidePlan& plan, hipStream_t stream) {
   if (p.elem == kElemF16) launch_elem<kElemF16>(p, plan, stream);
   else if (p.elem == kElemBf16) launch_elem<kElemBf16>(p, plan, stream);
   else launch_elem<kElemI8>(p, plan, stream);
