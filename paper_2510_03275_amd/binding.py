@@ -160,7 +160,18 @@ def _native_calls():
     return _sdqcall.linear, _sdqcall.linear_group, _sdqcall.linear_workspace_bytes
 
 
+def _native_dense_calls():
+    names = ("sdq_int8_linear", "sdq_int8_gated_linear", "sdq_gated_linear")
+    try:
+        from . import _sdqcall
+    except ImportError:
+        return [getattr(_lib, name) for name in names]      # no layouts: integers as they are
+    _sdqcall.bind_dense(*(ctypes.cast(getattr(_lib, n), ctypes.c_void_p).value for n in names))
+    return _sdqcall.int8_linear, _sdqcall.int8_gated_linear, _sdqcall.gated_linear
+
+
 _call_linear, _call_group, _call_workspace = _native_calls()
+_call_int8_linear, _call_int8_gated_linear, _call_gated_linear = _native_dense_calls()
 _addr = ctypes.addressof
 _DTYPES = {torch.float16: SDQ_F16, torch.bfloat16: SDQ_BF16, torch.float32: SDQ_F32}
 
@@ -389,10 +400,12 @@ def sdq_int8_linear_workspace_bytes(m: int, n: int, k: int) -> int:
 
 def sdq_int8_linear(x, w, w_scales, y, workspace, stream=None, accumulate: bool = False, x_scales=None) -> None:
     """y = x w^T for int8 w [n, k]; x is quantised by the call, or int8 codes with x_scales."""
-    _check(_lib.sdq_int8_linear(_ptr(x), SDQ_F16 if x_scales is not None else _dtype_code(x), _ptr(x_scales),
-                                x.shape[0], _ptr(w), _ptr(w_scales), w.shape[0], w.shape[1], _ptr(y),
-                                _dtype_code(y), int(bool(accumulate)), _ptr(workspace), _nbytes(workspace),
-                                _stream(stream)))
+    n, k = w.shape
+    status = _call_int8_linear(x.data_ptr(), SDQ_F16 if x_scales is not None else _DTYPES[x.dtype], _ptr(x_scales),
+                               x.shape[0], w.data_ptr(), w_scales.data_ptr(), n, k, y.data_ptr(), _DTYPES[y.dtype],
+                               1 if accumulate else 0, _ptr(workspace), _nbytes(workspace), _stream(stream))
+    if status != SDQ_OK:
+        _check(status)
 
 
 def sdq_int8_gated_linear_workspace_bytes(m: int, f: int, k: int) -> int:
@@ -402,10 +415,13 @@ def sdq_int8_gated_linear_workspace_bytes(m: int, f: int, k: int) -> int:
 def sdq_int8_gated_linear(x, gate, gate_scales, up, up_scales, act: int, h, workspace, stream=None,
                           x_scales=None) -> None:
     """h = act(x gate^T) * (x up^T) for int8 gate and up [f, k]; x as in sdq_int8_linear."""
-    _check(_lib.sdq_int8_gated_linear(_ptr(x), SDQ_F16 if x_scales is not None else _dtype_code(x), _ptr(x_scales),
-                                      x.shape[0], _ptr(gate), _ptr(gate_scales), _ptr(up), _ptr(up_scales),
-                                      gate.shape[0], gate.shape[1], int(act), _ptr(h), _dtype_code(h),
-                                      _ptr(workspace), _nbytes(workspace), _stream(stream)))
+    f, k = gate.shape
+    status = _call_int8_gated_linear(x.data_ptr(), SDQ_F16 if x_scales is not None else _DTYPES[x.dtype],
+                                     _ptr(x_scales), x.shape[0], gate.data_ptr(), gate_scales.data_ptr(),
+                                     up.data_ptr(), up_scales.data_ptr(), f, k, int(act), h.data_ptr(),
+                                     _DTYPES[h.dtype], _ptr(workspace), _nbytes(workspace), _stream(stream))
+    if status != SDQ_OK:
+        _check(status)
 
 
 def sdq_gated_linear_workspace_bytes(m: int, f: int, k: int) -> int:
@@ -414,9 +430,12 @@ def sdq_gated_linear_workspace_bytes(m: int, f: int, k: int) -> int:
 
 def sdq_gated_linear(x, gate, up, act: int, h, workspace, stream=None, g=None, u=None) -> None:
     """h = act(x gate^T) * (x up^T), all of x's type; g and u [m, f] also keep the projections."""
-    _check(_lib.sdq_gated_linear(_ptr(x), _dtype_code(x), x.shape[0], _ptr(gate), _ptr(up), gate.shape[0],
-                                 gate.shape[1], int(act), _ptr(h), _ptr(g), _ptr(u), _ptr(workspace),
-                                 _nbytes(workspace), _stream(stream)))
+    f, k = gate.shape
+    status = _call_gated_linear(x.data_ptr(), _DTYPES[x.dtype], x.shape[0], gate.data_ptr(), up.data_ptr(), f, k,
+                                int(act), h.data_ptr(), _ptr(g), _ptr(u), _ptr(workspace), _nbytes(workspace),
+                                _stream(stream))
+    if status != SDQ_OK:
+        _check(status)
 
 
 def sdq_gated_linear_backward_workspace_bytes(m: int, f: int, k: int) -> int:
@@ -568,32 +587,39 @@ class Int8Rows:
 
 
 _HALF = (torch.float16, torch.bfloat16)
+_FLOATS = tuple(_DTYPES)
+_INT8, _FLOAT32 = (torch.int8,), (torch.float32,)
 _current_device = torch.cuda.current_device
 
 
-def _matrix(name, t, shape, dtypes) -> None:
-    """t is a dense matrix of that shape on the current device, of one of the types."""
-    if not t.is_cuda or not t.is_contiguous() or t.shape != shape:
-        raise ValueError(f"{name} must be a contiguous device tensor {list(shape)}")
-    if t.dtype not in dtypes:
-        raise ValueError(f"{name} is {t.dtype}, not one of {', '.join(map(str, dtypes))}")
-    if t.device.index != _current_device():
-        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{_current_device()}")
+def _matrix(name, t, shape, dtypes, device) -> None:
+    """t is a dense matrix of that shape on the current device (its index), of one of the types."""
+    if t.get_device() != device or not t.is_contiguous() or t.shape != shape or t.dtype not in dtypes:
+        if not t.is_cuda or not t.is_contiguous() or t.shape != shape:
+            raise ValueError(f"{name} must be a contiguous device tensor {list(shape)}")
+        if t.dtype not in dtypes:
+            raise ValueError(f"{name} is {t.dtype}, not one of {', '.join(map(str, dtypes))}")
+        raise ValueError(f"{name} is on {t.device}, the current device is cuda:{device}")
 
 
-def _rows8(name, r: Int8Rows, shape) -> None:
-    _matrix(name + ".q", r.q, shape, (torch.int8,))
-    _matrix(name + ".scales", r.scales, shape[:1], (torch.float32,))
+def _device(t) -> int:
+    """The current device, for a tensor on one (without a GPU there is none to ask for)."""
+    return _current_device() if t.is_cuda else 0
 
 
-def _rows_in(x, k: int) -> int:
+def _rows8(name, r: Int8Rows, shape, device) -> None:
+    _matrix(name + ".q", r.q, shape, _INT8, device)
+    _matrix(name + ".scales", r.scales, shape[:1], _FLOAT32, device)
+
+
+def _rows_in(x, k: int, device) -> int:
     """Rows of an activation that is a float matrix or Int8Rows, after its checks."""
     if isinstance(x, Int8Rows):
         m = x.q.shape[0] if x.q.dim() == 2 else 0
-        _rows8("x", x, (m, k))
+        _rows8("x", x, (m, k), device)
         return m
     m = x.shape[0] if x.dim() == 2 else 0
-    _matrix("x", x, (m, k), tuple(_DTYPES))
+    _matrix("x", x, (m, k), _FLOATS, device)
     return m
 
 
@@ -605,22 +631,28 @@ def _empty(shape, dtype, device, stream=None):
         return torch.empty(shape, dtype=dtype, device=device)
 
 
-def _workspace(workspace, need: int, device, stream):
-    """The workspace given if it is large enough, else one of the call's own."""
-    if workspace is not None and workspace.nbytes >= need:
-        return workspace
-    return _empty(need, torch.uint8, device, stream) if need else None
+def _with_workspace(call, workspace, need, device, stream) -> None:
+    """call(workspace) with the one given if it is large enough, else with one of need() bytes."""
+    if workspace is not None:
+        try:
+            return call(workspace)
+        except SdqError as e:          # raised before anything is launched
+            if e.status != SDQ_ERR_WORKSPACE:
+                raise
+    n = need()
+    call(_empty(n, torch.uint8, device, stream) if n else None)
 
 
 def int8_quantize(x, out: Optional[Int8Rows] = None, stream=None) -> Int8Rows:
     """8-bit codes and a scale for every row of a device matrix [m, k] (fp16, bf16 or fp32):
     activations per token, or weights per output channel."""
     m, k = x.shape if x.dim() == 2 else (0, 0)
-    _matrix("x", x, (m, k), tuple(_DTYPES))
+    dev = _device(x)
+    _matrix("x", x, (m, k), _FLOATS, dev)
     if out is None:
         out = Int8Rows(_empty((m, k), torch.int8, x.device, stream), _empty((m,), torch.float32, x.device, stream))
     else:
-        _rows8("out", out, (m, k))
+        _rows8("out", out, (m, k), dev)
     sdq_int8_quantize(x, out.q, out.scales, stream)
     return out
 
@@ -636,19 +668,18 @@ def int8_linear(x, w: Int8Rows, workspace=None, out=None, stream=None, accumulat
     if w.q.dim() != 2:
         raise ValueError("w.q must be a matrix [n, k]")
     n, k = w.q.shape
-    _rows8("w", w, (n, k))
-    m = _rows_in(x, k)
+    dev = _device(w.q)
+    _rows8("w", w, (n, k), dev)
+    m = _rows_in(x, k, dev)
     codes = isinstance(x, Int8Rows)
     if out is None:
         if accumulate:
             raise ValueError("accumulate=True needs out")
         out = _empty((m, n), dtype or (torch.float16 if codes else x.dtype), w.q.device, stream)
-    _matrix("out", out, (m, n), tuple(_DTYPES) if dtype is None else (dtype,))
-    ws = _workspace(workspace, sdq_int8_linear_workspace_bytes(m, n, k), w.q.device, stream)
-    if codes:
-        sdq_int8_linear(x.q, w.q, w.scales, out, ws, stream, accumulate, x.scales)
-    else:
-        sdq_int8_linear(x, w.q, w.scales, out, ws, stream, accumulate)
+    _matrix("out", out, (m, n), _FLOATS if dtype is None else (dtype,), dev)
+    _with_workspace(lambda ws: sdq_int8_linear(x.q if codes else x, w.q, w.scales, out, ws, stream, accumulate,
+                                               x.scales if codes else None),
+                    workspace, lambda: sdq_int8_linear_workspace_bytes(m, n, k), w.q.device, stream)
     return out
 
 
@@ -658,18 +689,17 @@ def int8_gated_linear(x, gate: Int8Rows, up: Int8Rows, act: int = SDQ_ACT_SILU, 
     if gate.q.dim() != 2:
         raise ValueError("gate.q must be a matrix [f, k]")
     f, k = gate.q.shape
-    _rows8("gate", gate, (f, k))
-    _rows8("up", up, (f, k))
-    m = _rows_in(x, k)
+    dev = _device(gate.q)
+    _rows8("gate", gate, (f, k), dev)
+    _rows8("up", up, (f, k), dev)
+    m = _rows_in(x, k, dev)
     codes = isinstance(x, Int8Rows)
     if out is None:
         out = _empty((m, f), dtype or (torch.float16 if codes else x.dtype), gate.q.device, stream)
-    _matrix("out", out, (m, f), tuple(_DTYPES) if dtype is None else (dtype,))
-    ws = _workspace(workspace, sdq_int8_gated_linear_workspace_bytes(m, f, k), gate.q.device, stream)
-    if codes:
-        sdq_int8_gated_linear(x.q, gate.q, gate.scales, up.q, up.scales, act, out, ws, stream, x.scales)
-    else:
-        sdq_int8_gated_linear(x, gate.q, gate.scales, up.q, up.scales, act, out, ws, stream)
+    _matrix("out", out, (m, f), _FLOATS if dtype is None else (dtype,), dev)
+    _with_workspace(lambda ws: sdq_int8_gated_linear(x.q if codes else x, gate.q, gate.scales, up.q, up.scales, act,
+                                                     out, ws, stream, x.scales if codes else None),
+                    workspace, lambda: sdq_int8_gated_linear_workspace_bytes(m, f, k), gate.q.device, stream)
     return out
 
 
@@ -680,15 +710,16 @@ def gated_linear(x, gate, up, act: int = SDQ_ACT_SILU, workspace=None, out=None,
     m, k = x.shape if x.dim() == 2 else (0, 0)
     f = gate.shape[0] if gate.dim() == 2 else 0
     t = (x.dtype,)
-    _matrix("x", x, (m, k), _HALF)
-    _matrix("gate", gate, (f, k), t)
-    _matrix("up", up, (f, k), t)
+    dev = _device(x)
+    _matrix("x", x, (m, k), _HALF, dev)
+    _matrix("gate", gate, (f, k), t, dev)
+    _matrix("up", up, (f, k), t, dev)
     for name, v in (("out", out), ("g", g), ("u", u)):
         if v is not None:
-            _matrix(name, v, (m, f), t)
+            _matrix(name, v, (m, f), t, dev)
     h = out if out is not None else _empty((m, f), x.dtype, x.device, stream)
-    ws = _workspace(workspace, sdq_gated_linear_workspace_bytes(m, f, k), x.device, stream)
-    sdq_gated_linear(x, gate, up, act, h, ws, stream, g, u)
+    _with_workspace(lambda ws: sdq_gated_linear(x, gate, up, act, h, ws, stream, g, u), workspace,
+                    lambda: sdq_gated_linear_workspace_bytes(m, f, k), x.device, stream)
     return h
 
 
@@ -703,26 +734,28 @@ def gated_linear_backward(dh, x, gate, up, g, u, act: int = SDQ_ACT_SILU, worksp
     m, k = x.shape if x.dim() == 2 else (0, 0)
     f = gate.shape[0] if gate.dim() == 2 else 0
     t = (x.dtype,)
-    _matrix("x", x, (m, k), _HALF)
-    _matrix("gate", gate, (f, k), t)
-    _matrix("up", up, (f, k), t)
+    dev = _device(x)
+    _matrix("x", x, (m, k), _HALF, dev)
+    _matrix("gate", gate, (f, k), t, dev)
+    _matrix("up", up, (f, k), t, dev)
     for name, v in (("dh", dh), ("g", g), ("u", u)):
-        _matrix(name, v, (m, f), t)
+        _matrix(name, v, (m, f), t, dev)
     if accumulate and need_weights and (dgate is None or dup is None):
         raise ValueError("accumulate=True needs dgate and dup")
     empty = lambda shape: _empty(shape, x.dtype, x.device, stream)
     if need_dx:
         dx = empty((m, k)) if dx is None else dx
-        _matrix("dx", dx, (m, k), t)
+        _matrix("dx", dx, (m, k), t, dev)
     else:
         dx = None
     if need_weights:
         dgate = empty((f, k)) if dgate is None else dgate
         dup = empty((f, k)) if dup is None else dup
-        _matrix("dgate", dgate, (f, k), t)
-        _matrix("dup", dup, (f, k), t)
+        _matrix("dgate", dgate, (f, k), t, dev)
+        _matrix("dup", dup, (f, k), t, dev)
     else:
         dgate = dup = None
-    ws = _workspace(workspace, sdq_gated_linear_backward_workspace_bytes(m, f, k), x.device, stream)
-    sdq_gated_linear_backward(dh, x, gate, up, act, g, u, dx, dgate, dup, ws, stream, accumulate)
+    _with_workspace(lambda ws: sdq_gated_linear_backward(dh, x, gate, up, act, g, u, dx, dgate, dup, ws, stream,
+                                                         accumulate),
+                    workspace, lambda: sdq_gated_linear_backward_workspace_bytes(m, f, k), x.device, stream)
     return dx, dgate, dup

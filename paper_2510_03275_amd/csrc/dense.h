@@ -55,10 +55,12 @@ sdq_status launch_product(const Product& p, hipStream_t stream);
 // The kernels behind it.  At most 64 rows, neither operand strided, rows at any alignment
 // (dense_few.hip):
 void launch_few(const Product& p, hipStream_t stream);
+double few_us(const Product& p);      // about what it takes
 // Tiles of 256 rows of wide, rows aligned (dense_wide.hip): how many rows of tall to a tile, and into
 // how many parts the depth is cut, whose sums take wide_part_bytes of the workspace.
 struct WidePlan {
   int tall = 256, splits = 0;
+  double us = 0;                      // about what it takes
 };
 WidePlan wide_plan(const Product& p);
 size_t wide_part_bytes(const Product& p, int splits);

@@ -26,7 +26,7 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Product p) {
   using S = typename E::Scalar;
   using Acc = typename E::Acc;
   constexpr int kPer = 16 / E::kBytes, kStep = 64 / E::kBytes;
-  constexpr int kDeep = TALL == 1 ? 4 : 2;                  // steps of 64 bytes per buffer
+  constexpr int kDeep = 2;                                  // steps of 64 bytes per buffer (3, 4 and 8: no faster)
   constexpr int kColTiles = GATED ? TILES / 2 : TILES;      // of 16 output columns
   __shared__ Acc part[WAVES / 2][TILES][TALL][64];
   const int tid = threadIdx.x, lane = tid % 64;
@@ -157,6 +157,13 @@ void launch_rows(const Product& p, hipStream_t stream) {
 }
 
 }  // namespace
+
+// Fitted as wide_plan's times are, up to 15 % off at 16 rows: 4 us and the weights at 4.9 TB/s, longer by
+// the rows' own reads, which from 17 rows on are more than the weights'.
+double few_us(const Product& p) {
+  const double bytes = static_cast<double>(p.cols) * p.depth * (p.gated ? 2 : 1) * (p.elem == kElemI8 ? 1 : 2);
+  return 4.0 + bytes / 4.9e6 * (1 + 0.015 * p.rows) * (p.rows > 16 ? 1.8 : 1.0);
+}
 
 void launch_few(const Product& p, hipStream_t stream) {
   if (p.elem == kElemF16) launch_rows<kElemF16>(p, stream);

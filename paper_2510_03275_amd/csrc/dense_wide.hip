@@ -444,27 +444,26 @@ size_t wide_part_bytes(const Product& p, int splits) {
 // within 10 % of the fastest of them but for single cases):
 //   a launch 2.5 us; a turn of the chip 2, 3.5 or 7.5 us for its first copies and its outputs and
 //   0.62, 0.72 or 1.1 us per step at 64, 128 or 256 rows of tall, up to 45 % more with every compute
-//   unit at work (power), or what the turn's rows of wide take from memory at 5.5 TB/s;
+//   unit at work (power), or what the turn's rows of wide take from memory at 5 TB/s;
 //   the partial sums 2.5 us and their bytes, written and read, at 6 TB/s.
 WidePlan wide_plan(const Product& p) {
   const int64_t bytes = p.elem == kElemI8 ? 1 : 2, units = device_compute_units();
   const int64_t steps = (p.depth * bytes + 127) / 128 * p.segments;
   const int64_t col_tiles = (p.cols + (p.gated ? 127 : 255)) / (p.gated ? 128 : 256) * p.batch;
   WidePlan best;
-  double best_us = 0;
   for (int tall = 256; tall >= (p.tall_strided ? 128 : 64); tall /= 2) {
     const int64_t tiles = col_tiles * ((p.rows + tall - 1) / tall);
     const double step = tall == 256 ? 1.1 : tall == 128 ? 0.72 : 0.62, ends = tall == 256 ? 7.5 : tall == 128 ? 3.5 : 2.0;
     for (int splits = 1; splits <= 32 && (splits == 1 || steps / splits >= 3); ++splits) {
       const int64_t at_once = std::min(tiles * splits, units), turns = (tiles * splits + units - 1) / units;
       const double busy = static_cast<double>(at_once) / units;
-      const double memory = std::min(col_tiles * splits, at_once) * 32768.0 / 5.5e6;
+      const double memory = std::min(col_tiles * splits, at_once) * 32768.0 / 5e6;
       double us = 2.5 + turns * (ends + (steps + splits - 1) / splits * std::max(step * (1 + 0.45 * busy), memory));
       if (splits > 1) us += 2.5 + wide_part_bytes(p, splits) * 2 / 6e6;
-      if (best.splits == 0 || us < best_us) {
+      if (best.splits == 0 || us < best.us) {
         best.tall = tall;
         best.splits = splits;
-        best_us = us;
+        best.us = us;
       }
     }
   }

@@ -83,11 +83,77 @@ static PyObject* py_ws(PyObject* self, PyObject* const* args, Py_ssize_t n) {
   return PyLong_FromSize_t(p_ws(PTR(const sdq_layout*, 0), (int64_t)a[1]));
 }
 
+/* The dense operators' per-token entry points. */
+typedef sdq_status (*int8_fn)(const void*, sdq_dtype, const float*, int64_t, const int8_t*, const float*, int64_t, int64_t,
+                              void*, sdq_dtype, int32_t, void*, size_t, void*);
+typedef sdq_status (*int8_gated_fn)(const void*, sdq_dtype, const float*, int64_t, const int8_t*, const float*,
+                                    const int8_t*, const float*, int64_t, int64_t, int32_t, void*, sdq_dtype, void*,
+                                    size_t, void*);
+typedef sdq_status (*gated_fn)(const void*, sdq_dtype, int64_t, const void*, const void*, int64_t, int64_t, int32_t, void*,
+                               void*, void*, void*, size_t, void*);
+
+static int8_fn p_int8;
+static int8_gated_fn p_int8_gated;
+static gated_fn p_gated;
+
+static PyObject* py_bind_dense(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  unsigned long long a[3];
+  (void)self;
+  if (take(args, n, 3, a)) return NULL;
+  p_int8 = (int8_fn)(uintptr_t)a[0];
+  p_int8_gated = (int8_gated_fn)(uintptr_t)a[1];
+  p_gated = (gated_fn)(uintptr_t)a[2];
+  Py_RETURN_NONE;
+}
+
+static PyObject* py_int8_linear(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  unsigned long long a[14];
+  sdq_status st;
+  (void)self;
+  if (take(args, n, 14, a)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  st = p_int8(PTR(const void*, 0), (sdq_dtype)a[1], PTR(const float*, 2), (int64_t)a[3], PTR(const int8_t*, 4),
+              PTR(const float*, 5), (int64_t)a[6], (int64_t)a[7], PTR(void*, 8), (sdq_dtype)a[9], (int32_t)a[10],
+              PTR(void*, 11), (size_t)a[12], PTR(void*, 13));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong((long)st);
+}
+
+static PyObject* py_int8_gated_linear(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  unsigned long long a[16];
+  sdq_status st;
+  (void)self;
+  if (take(args, n, 16, a)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  st = p_int8_gated(PTR(const void*, 0), (sdq_dtype)a[1], PTR(const float*, 2), (int64_t)a[3], PTR(const int8_t*, 4),
+                    PTR(const float*, 5), PTR(const int8_t*, 6), PTR(const float*, 7), (int64_t)a[8], (int64_t)a[9],
+                    (int32_t)a[10], PTR(void*, 11), (sdq_dtype)a[12], PTR(void*, 13), (size_t)a[14], PTR(void*, 15));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong((long)st);
+}
+
+static PyObject* py_gated_linear(PyObject* self, PyObject* const* args, Py_ssize_t n) {
+  unsigned long long a[14];
+  sdq_status st;
+  (void)self;
+  if (take(args, n, 14, a)) return NULL;
+  Py_BEGIN_ALLOW_THREADS
+  st = p_gated(PTR(const void*, 0), (sdq_dtype)a[1], (int64_t)a[2], PTR(const void*, 3), PTR(const void*, 4),
+               (int64_t)a[5], (int64_t)a[6], (int32_t)a[7], PTR(void*, 8), PTR(void*, 9), PTR(void*, 10), PTR(void*, 11),
+               (size_t)a[12], PTR(void*, 13));
+  Py_END_ALLOW_THREADS
+  return PyLong_FromLong((long)st);
+}
+
 static PyMethodDef methods[] = {
     {"bind", (PyCFunction)(void (*)(void))py_bind, METH_FASTCALL, "addresses of the library's functions"},
     {"linear", (PyCFunction)(void (*)(void))py_linear, METH_FASTCALL, "sdq_linear"},
     {"linear_group", (PyCFunction)(void (*)(void))py_group, METH_FASTCALL, "sdq_linear_group"},
     {"linear_workspace_bytes", (PyCFunction)(void (*)(void))py_ws, METH_FASTCALL, "sdq_linear_workspace_bytes"},
+    {"bind_dense", (PyCFunction)(void (*)(void))py_bind_dense, METH_FASTCALL, "addresses of the dense operators"},
+    {"int8_linear", (PyCFunction)(void (*)(void))py_int8_linear, METH_FASTCALL, "sdq_int8_linear"},
+    {"int8_gated_linear", (PyCFunction)(void (*)(void))py_int8_gated_linear, METH_FASTCALL, "sdq_int8_gated_linear"},
+    {"gated_linear", (PyCFunction)(void (*)(void))py_gated_linear, METH_FASTCALL, "sdq_gated_linear"},
     {NULL, NULL, 0, NULL},
 };
 
