@@ -33,6 +33,9 @@ struct Product {
   // 8-bit operands: a scale per row of tall and per row of wide
   const float* tall_scale = nullptr;
   const float* wide_scale[2] = {};
+  // 8-bit: rows not yet quantised (tall and tall_scale are not read then), for the kernel that does it
+  const void* x = nullptr;
+  int x_type = SDQ_F16;
   // Output [rows][cols] of type out_type; accumulate: added into.
   void* out[2] = {};
   int out_type = SDQ_F16;
@@ -51,10 +54,13 @@ size_t product_ws_bytes(const Product& p);
 // is; elements past n are then zeros (depth-contiguous) or anything (strided).
 int64_t product_ld(const Product& p, int64_t n);
 sdq_status launch_product(const Product& p, hipStream_t stream);
+// Whether launch_product quantises the rows of an 8-bit product itself, if given x.
+bool product_quantizes(const Product& p);
 
 // The kernels behind it.  At most 64 rows, neither operand strided, rows at any alignment
 // (dense_few.hip):
 void launch_few(const Product& p, hipStream_t stream);
+bool few_quantizes(const Product& p);
 double few_us(const Product& p);      // about what it takes
 // Tiles of 256 rows of wide, rows aligned (dense_wide.hip): how many rows of tall to a tile, and into
 // how many parts the depth is cut, whose sums take wide_part_bytes of the workspace.

@@ -93,6 +93,9 @@ sdq_status run_int8(Product p, const void* x, sdq_dtype xt, const float* x_scale
   if (x_scales) {
     p.tall[0] = x;
     p.tall_scale = x_scales;
+  } else if (product_quantizes(p)) {
+    p.x = x;
+    p.x_type = xt;
   } else {
     const int64_t ld = product_ld(p, p.depth);
     st = launch_int8_quantize(x, xt, p.rows, p.depth, s.q, ld, s.scales, stream);

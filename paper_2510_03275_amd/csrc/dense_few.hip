@@ -11,16 +11,70 @@
 // the same way, rows past the last as copies of it whose outputs are not
 // stored.  Rows need not start aligned: only the bytes behind the last whole
 // step are read element by element.
+//
+// A small call on 8-bit weights quantises its rows itself: every workgroup forms the codes of all rows
+// in LDS while its first weights are on their way, which saves the launch of
+// sdq_int8_quantize's kernel and its memory round trip (one row against 768 x 768 in 3.9 us instead of
+// 5.6, 1024 x 16384 in 13.6 instead of 16.7; of several rows only short ones: 3 of 1001 in 5.8 instead
+// of 7.8, but 16 of 768 would take 9.2 instead of 6.2 and 4 of 4096 11.1 instead of 10.6).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
 
-#include "dense_device.h"
+#include "dense_quantize.h"
 
 namespace sdq {
 namespace {
 
-template <int ELEM, bool GATED, int TILES, int TALL, int WAVES>
+constexpr int kOwnCodes = 16384;                // codes of all rows that a workgroup forms itself
+constexpr int kOwnBytes = kOwnCodes + 16 * 32;  // in LDS: rows 16-byte aligned and 16 bytes apart (banks)
+
+// The codes and scales of all rows (at least 16 elements, 16 rows at most), each row by a group of the
+// workgroup's waves, to LDS.
+template <int XT, int WAVES>
+__device__ inline void quantize_own(const Product& p, int8_t* codes, int ld, float* scales, int wave, int lane) {
+  using X = typename Out<XT>::Scalar;
+  constexpr int kPer = 16 / sizeof(X);
+  __shared__ uint32_t largest[WAVES];
+  const int rows = static_cast<int>(p.rows), k = static_cast<int>(p.depth);
+  const int group = rows >= WAVES ? 1 : WAVES / rows, groups = WAVES / group;      // waves to a row, rows at once
+  const int mine = wave % group * 64 + lane, chunks = (k + kPer - 1) / kPer;
+  for (int r0 = 0; r0 < rows; r0 += groups) {
+    const int r = r0 + wave / group;
+    const bool on = wave / group < groups && r < rows;
+    const X* src = static_cast<const X*>(p.x) + static_cast<int64_t>(on ? r : 0) * k;
+    uint32_t a = 0;
+    for (int c = mine; on && c < chunks; c += 64 * group) {      // the last chunk starts early, as in whole rows
+      u32x4 v;
+      __builtin_memcpy(&v, src + min(c * kPer, k - kPer), 16);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) a = larger<X>(a, v[j]);
+    }
+#pragma unroll
+    for (int off = 32; off > 0; off /= 2) a = larger<X>(a, __shfl_xor(a, off, 64));
+    if (lane == 0) largest[wave] = a;
+    __syncthreads();
+    if (on) {
+      for (int g = 0; g < group; ++g) a = larger<X>(a, largest[wave - wave % group + g]);
+      const float top = magnitude<X>(a);
+      const bool finite = top <= kLargestFloat;
+      const float s = row_scale(top), inv = 1.0f / s;
+      if (mine == 0) scales[r] = finite ? s : __builtin_nanf("");
+      for (int c = mine; c < chunks; c += 64 * group) {
+        const int at = min(c * kPer, k - kPer);
+        u32x4 v;
+        __builtin_memcpy(&v, src + at, 16);
+        uint32_t o[kPer / 4] = {};
+        if (finite) quantize_chunk<X>(v, s, inv, o);
+        __builtin_memcpy(codes + r * ld + at, o, kPer);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// XT: the type of the rows that the call quantises itself, or -1 (rows of the products' own type).
+template <int ELEM, bool GATED, int TILES, int TALL, int WAVES, int XT>
 __global__ __launch_bounds__(64 * WAVES) void few_kernel(Product p) {
   using E = Elem<ELEM>;
   using S = typename E::Scalar;
@@ -35,9 +89,14 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Product p) {
   const int64_t i = lane % 16, c = (lane / 16) * kPer;
   const S* x[TALL];
   const S* w[TILES];
+  constexpr bool kOwn = XT >= 0;
+  __shared__ __attribute__((aligned(16))) int8_t codes[kOwn ? kOwnBytes : 16];
+  __shared__ float own_scales[16];
+  const int own_ld = static_cast<int>((p.depth + 15) / 16 * 16) + 16;
 #pragma unroll
   for (int j = 0; j < TALL; ++j)
-    x[j] = static_cast<const S*>(p.tall[0]) + min(16 * j + i, p.rows - 1) * p.ld_tall + c;
+    x[j] = kOwn ? reinterpret_cast<const S*>(codes) + min(i, p.rows - 1) * own_ld + c
+                : static_cast<const S*>(p.tall[0]) + min(16 * j + i, p.rows - 1) * p.ld_tall + c;
 #pragma unroll
   for (int t = 0; t < TILES; ++t)
     w[t] = static_cast<const S*>(p.wide[t / kColTiles]) + min(col0 + 16 * (t % kColTiles) + i, p.cols - 1) * p.ld_wide + c;
@@ -47,15 +106,26 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Product p) {
 
   Acc acc[TILES][TALL] = {};
   i32x4 wv[2][kDeep][TILES], xv[2][kDeep][TALL];
-  auto fetch = [&](int b, int s) {      // kDeep steps from s on; steps past the end repeat the last one
+  // kDeep steps from s on; steps past the end repeat the last one.
+  auto fetch_wide = [&](int b, int s) {
 #pragma unroll
     for (int d = 0; d < kDeep; ++d) {
       const int64_t at = static_cast<int64_t>(min(s + d, s1 - 1)) * kStep;
 #pragma unroll
       for (int t = 0; t < TILES; ++t) __builtin_memcpy(&wv[b][d][t], w[t] + at, 16);
+    }
+  };
+  auto fetch_tall = [&](int b, int s) {
+#pragma unroll
+    for (int d = 0; d < kDeep; ++d) {
+      const int64_t at = static_cast<int64_t>(min(s + d, s1 - 1)) * kStep;
 #pragma unroll
       for (int j = 0; j < TALL; ++j) __builtin_memcpy(&xv[b][d][j], x[j] + at, 16);
     }
+  };
+  auto fetch = [&](int b, int s) {
+    fetch_wide(b, s);
+    fetch_tall(b, s);
   };
   auto multiply = [&](int b, int s) {
 #pragma unroll
@@ -66,8 +136,10 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Product p) {
 #pragma unroll
           for (int j = 0; j < TALL; ++j) acc[t][j] = E::mfma(wv[b][d][t], xv[b][d][j], acc[t][j]);
   };
+  if (s0 < s1) fetch_wide(0, s0);
+  if constexpr (kOwn) quantize_own<XT, WAVES>(p, codes, own_ld, own_scales, wave, lane);
   if (s0 < s1) {
-    fetch(0, s0);
+    fetch_tall(0, s0);
     for (int s = s0; s < s1; s += 2 * kDeep) {
       fetch(1, s + kDeep);
       multiply(0, s);
@@ -123,40 +195,55 @@ __global__ __launch_bounds__(64 * WAVES) void few_kernel(Product p) {
     with_out_type<ELEM>(p, [&](auto type) {
       finish4<ELEM, GATED, decltype(type)::value>(p, 0, row, r, part[0][t][j][lane],
                                                   part[0][GATED ? kColTiles + t : t][j][lane],
-                                                  ELEM == kElemI8 ? p.tall_scale[row] : 1.0f, sw);
+                                                  kOwn ? own_scales[row % 16] : ELEM == kElemI8 ? p.tall_scale[row] : 1.0f, sw);
     });
   }
 }
 
-template <int ELEM, bool GATED, int TILES, int TALL>
+template <int ELEM, bool GATED, int TILES, int TALL, int XT>
 void launch_waves(const Product& p, hipStream_t stream) {
   constexpr int64_t kPer = GATED ? 8 * TILES : 16 * TILES;
   const dim3 grid(static_cast<unsigned>((p.cols + kPer - 1) / kPer));
   // Waves enough for eight per compute unit in all, each with some steps of its own at least.
   const int64_t steps = p.depth * Elem<ELEM>::kBytes / 64, units = device_compute_units();
   if (grid.x * 4 >= 8 * units || steps < 16) {
-    few_kernel<ELEM, GATED, TILES, TALL, 4><<<grid, 256, 0, stream>>>(p);
+    few_kernel<ELEM, GATED, TILES, TALL, 4, XT><<<grid, 256, 0, stream>>>(p);
   } else if (TALL > 1 || grid.x * 8 >= 8 * units || steps < 64) {
-    few_kernel<ELEM, GATED, TILES, TALL, 8><<<grid, 512, 0, stream>>>(p);
+    few_kernel<ELEM, GATED, TILES, TALL, 8, XT><<<grid, 512, 0, stream>>>(p);
   } else if constexpr (TALL == 1) {
-    few_kernel<ELEM, GATED, TILES, TALL, 16><<<grid, 1024, 0, stream>>>(p);
+    few_kernel<ELEM, GATED, TILES, TALL, 16, XT><<<grid, 1024, 0, stream>>>(p);
   }
+}
+
+template <int ELEM, bool GATED, int TILES>
+void launch_16(const Product& p, hipStream_t stream) {
+  if constexpr (ELEM == kElemI8) {
+    if (p.x && p.x_type == SDQ_F16) return launch_waves<ELEM, GATED, TILES, 1, SDQ_F16>(p, stream);
+    if (p.x && p.x_type == SDQ_BF16) return launch_waves<ELEM, GATED, TILES, 1, SDQ_BF16>(p, stream);
+    if (p.x) return launch_waves<ELEM, GATED, TILES, 1, SDQ_F32>(p, stream);
+  }
+  launch_waves<ELEM, GATED, TILES, 1, -1>(p, stream);
 }
 
 template <int ELEM>
 void launch_rows(const Product& p, hipStream_t stream) {
   if (p.gated) {
-    if (p.rows <= 16) launch_waves<ELEM, true, 2, 1>(p, stream);
-    else if (p.rows <= 32) launch_waves<ELEM, true, 4, 2>(p, stream);
-    else launch_waves<ELEM, true, 4, 4>(p, stream);
+    if (p.rows <= 16) launch_16<ELEM, true, 2>(p, stream);
+    else if (p.rows <= 32) launch_waves<ELEM, true, 4, 2, -1>(p, stream);
+    else launch_waves<ELEM, true, 4, 4, -1>(p, stream);
   } else if constexpr (ELEM == kElemI8) {
-    if (p.rows <= 16) launch_waves<ELEM, false, 1, 1>(p, stream);
-    else if (p.rows <= 32) launch_waves<ELEM, false, 2, 2>(p, stream);
-    else launch_waves<ELEM, false, 2, 4>(p, stream);
+    if (p.rows <= 16) launch_16<ELEM, false, 1>(p, stream);
+    else if (p.rows <= 32) launch_waves<ELEM, false, 2, 2, -1>(p, stream);
+    else launch_waves<ELEM, false, 2, 4, -1>(p, stream);
   }
 }
 
 }  // namespace
+
+bool few_quantizes(const Product& p) {
+  return p.elem == kElemI8 && p.rows <= 16 && p.depth >= 16 &&
+         p.rows * p.depth <= (p.rows == 1 ? kOwnCodes : kOwnCodes / 4);
+}
 
 // Fitted as wide_plan's times are, up to 15 % off at 16 rows: 4 us and the weights at 4.9 TB/s, longer by
 // the rows' own reads, which from 17 rows on are more than the weights'.

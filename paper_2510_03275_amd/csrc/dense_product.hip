@@ -120,6 +120,8 @@ void pad_rows(const void* src, int64_t rows, int64_t ld, void* dst, int64_t ld_d
 
 int64_t product_ld(const Product& p, int64_t n) { return takes_few(p) ? n : aligned_ld(p, n); }
 
+bool product_quantizes(const Product& p) { return takes_few(p) && few_quantizes(p); }
+
 size_t product_ws_bytes(const Product& p) {
   return takes_few(p) || p.rows == 0 || p.cols == 0 ? 0 : product_space(p, wide_plan(p), nullptr).bytes;
 }
