@@ -66,6 +66,7 @@ double few_us(const Product& p);      // about what it takes
 // how many parts the depth is cut, whose sums take wide_part_bytes of the workspace.
 struct WidePlan {
   int tall = 256, splits = 0;
+  int64_t mixed = 0;                  // tiles of 256 rows for so many of them, of 128 for the rest
   double us = 0;                      // about what it takes
 };
 WidePlan wide_plan(const Product& p);

@@ -10,24 +10,45 @@
 namespace sdq {
 namespace {
 
-// Rows of `len` bytes copied to rows of ld bytes (a multiple of 16), the rest of them zeros.
-// A thread writes 16 bytes, from two 16-byte reads at most one of which is unaligned.
-__global__ __launch_bounds__(256) void pad_rows_kernel(const char* __restrict__ src, int64_t rows, int64_t len,
-                                                       char* __restrict__ dst, int64_t ld) {
-  const int64_t per = ld / 16, n = rows * per;
-  for (int64_t o = blockIdx.x * int64_t{256} + threadIdx.x; o < n; o += gridDim.x * int64_t{256}) {
-    const int64_t row = o / per, c = (o - row * per) * 16;
-    const char* at = src + row * len + c;
-    i32x4 v = {0, 0, 0, 0};
-    if (c + 16 <= len) {
-      __builtin_memcpy(&v, at, 16);
-    } else {
-      char e[16];
+// Up to four matrices of rows of `len` bytes copied to rows of ld bytes (a multiple of 16), the rest of
+// them zeros, in one launch.  A thread writes 16 bytes.
+struct PadJob {
+  const char* src = nullptr;
+  char* dst = nullptr;
+  int64_t len = 0, ld = 0, chunks = 0;      // chunks: of 16 bytes, in all rows
+};
+struct PadJobs {
+  PadJob of[4];
+  int count = 0;
+};
+// o / per and the rest, in 32 bits where that is enough (a 64-bit division is a hundred instructions).
+__device__ inline int64_t divide(int64_t o, int64_t per, int64_t* rest) {
+  int64_t q;
+  if ((o | per) >> 32 == 0) q = static_cast<unsigned>(o) / static_cast<unsigned>(per);
+  else q = o / per;
+  *rest = o - q * per;
+  return q;
+}
+__global__ __launch_bounds__(256) void pad_rows_kernel(PadJobs jobs) {
+  for (int n = 0; n < jobs.count; ++n) {
+    const PadJob& job = jobs.of[n];
+    const int64_t per = job.ld / 16;
+    for (int64_t o = blockIdx.x * int64_t{256} + threadIdx.x; o < job.chunks; o += gridDim.x * int64_t{256}) {
+      int64_t c;
+      const int64_t row = divide(o, per, &c);
+      c *= 16;
+      const char* at = job.src + row * job.len + c;
+      i32x4 v = {0, 0, 0, 0};
+      if (c + 16 <= job.len) {
+        __builtin_memcpy(&v, at, 16);
+      } else {
+        char e[16];
 #pragma unroll
-      for (int j = 0; j < 16; ++j) e[j] = c + j < len ? at[j] : char(0);
-      __builtin_memcpy(&v, e, 16);
+        for (int j = 0; j < 16; ++j) e[j] = c + j < job.len ? at[j] : char(0);
+        __builtin_memcpy(&v, e, 16);
+      }
+      *reinterpret_cast<i32x4*>(job.dst + 16 * o) = v;
     }
-    *reinterpret_cast<i32x4*>(dst + 16 * o) = v;
   }
 }
 
@@ -38,7 +59,10 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict_
                                                             int act, S* __restrict__ dg, S* __restrict__ du) {
   const int64_t o = blockIdx.x * int64_t{256} + threadIdx.x, per = ld / 8;
   if (o >= m * per) return;
-  const int64_t row = o / per, c = (o - row * per) * 8, i = row * f + c;
+  int64_t c;
+  const int64_t row = divide(o, per, &c);
+  c *= 8;
+  const int64_t i = row * f + c;
   S a[8], b[8], d[8], x[8], y[8];
   if (c + 8 <= f) {      // rows of f elements need not start aligned
     __builtin_memcpy(a, dh + i, 16);
@@ -108,12 +132,17 @@ Space product_space(const Product& p, const WidePlan& plan, void* ws) {
   return s;
 }
 
-void pad_rows(const void* src, int64_t rows, int64_t ld, void* dst, int64_t ld_dst, int64_t b, hipStream_t stream) {
-  const int64_t n = rows * ld_dst * b / 16;
-  if (n == 0) return;
-  const dim3 grid(static_cast<unsigned>(std::min<int64_t>((n + 255) / 256, 1 << 16)));
-  pad_rows_kernel<<<grid, 256, 0, stream>>>(static_cast<const char*>(src), rows, ld * b, static_cast<char*>(dst),
-                                            ld_dst * b);
+void add_pad(PadJobs* jobs, const void* src, int64_t rows, int64_t ld, void* dst, int64_t ld_dst, int64_t b) {
+  if (rows == 0) return;
+  jobs->of[jobs->count++] = {static_cast<const char*>(src), static_cast<char*>(dst), ld * b, ld_dst * b,
+                             rows * ld_dst * b / 16};
+}
+
+void launch_pads(const PadJobs& jobs, hipStream_t stream) {
+  int64_t most = 0;
+  for (int n = 0; n < jobs.count; ++n) most = std::max(most, jobs.of[n].chunks);
+  if (most == 0) return;
+  pad_rows_kernel<<<dim3(static_cast<unsigned>(std::min<int64_t>((most + 255) / 256, 1 << 16))), 256, 0, stream>>>(jobs);
 }
 
 }  // namespace
@@ -134,16 +163,18 @@ sdq_status launch_product(const Product& given, hipStream_t stream) {
     const WidePlan plan = wide_plan(p);
     const Space s = product_space(p, plan, p.ws);
     const int64_t b = elem_bytes(p);
+    PadJobs pads;
     for (int i = 0; i < 2; ++i) {
       if (s.wide[i]) {
-        pad_rows(p.wide[i], p.wide_strided ? p.depth : p.cols, p.ld_wide, s.wide[i], s.ld_wide, b, stream);
+        add_pad(&pads, p.wide[i], p.wide_strided ? p.depth : p.cols, p.ld_wide, s.wide[i], s.ld_wide, b);
         p.wide[i] = s.wide[i];
       }
       if (s.tall[i]) {
-        pad_rows(p.tall[i], p.tall_strided ? p.depth : p.rows, p.ld_tall, s.tall[i], s.ld_tall, b, stream);
+        add_pad(&pads, p.tall[i], p.tall_strided ? p.depth : p.rows, p.ld_tall, s.tall[i], s.ld_tall, b);
         p.tall[i] = s.tall[i];
       }
     }
+    launch_pads(pads, stream);
     p.ld_wide = s.ld_wide;
     p.ld_tall = s.ld_tall;
     p.ws = s.parts;

@@ -200,8 +200,13 @@ template <> struct Stages<256> { static constexpr int kTall = 2, kWide = 3; };
 template <> struct Stages<128> { static constexpr int kTall = 3, kWide = 3; };
 template <> struct Stages<64> { static constexpr int kTall = 4, kWide = 4; };
 
+template <int TALL>
+constexpr int kLdsBytes = (Stages<TALL>::kTall * TALL + Stages<TALL>::kWide * 256) * kStepBytes;
+
+// One tile of the rows from first_row on, `index` of the `total` workgroups that share them.
 template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED, int TALL>
-__global__ __launch_bounds__(512, 2) void wide_kernel(Product p, int splits) {
+__device__ __forceinline__ void wide_tile(const Product& p, int splits, char* lds, int64_t first_row, int64_t rows,
+                                          unsigned index, unsigned total) {
   using E = Elem<ELEM>;
   using Acc = typename E::Acc;
   constexpr int kB = E::kBytes, kStep = kStepBytes / kB;
@@ -210,24 +215,23 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p, int splits) {
   constexpr int kWide = kTallStages * kTallStep, kEnd = kWide + kWideStages * kWideStep;
   constexpr int kFrags = TALL / 32;                 // of 16 rows of tall per wave
   constexpr int kTallCopies = TALL / 64, kWideCopies = 4;
-  __shared__ __attribute__((aligned(1024))) char lds[kEnd];   // stages of tall, of wide
+  static_assert(kEnd == kLdsBytes<TALL>, "stages of tall, then of wide");
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int ww = wave % 4, wt = wave / 4;
 
   constexpr int kCols = GATED ? 128 : 256;
   const unsigned nw = static_cast<unsigned>((p.cols + kCols - 1) / kCols);
-  const unsigned nt = static_cast<unsigned>((p.rows + TALL - 1) / TALL);
-  const unsigned total = gridDim.x, id = blockIdx.x;
-  const unsigned xcd = id % kXcds, per = total / kXcds, rem = total % kXcds;
-  unsigned tile = xcd * per + (xcd < rem ? xcd : rem) + id / kXcds;
+  const unsigned nt = static_cast<unsigned>((rows + TALL - 1) / TALL);
+  const unsigned xcd = index % kXcds, per = total / kXcds, rem = total % kXcds;
+  unsigned tile = xcd * per + (xcd < rem ? xcd : rem) + index / kXcds;
   const int part = __builtin_amdgcn_readfirstlane(tile / (nw * nt));
   tile -= part * (nw * nt);
   const int z = p.batch > 1 ? part % p.batch : 0, at = p.batch > 1 ? part / p.batch : part;   // output, part of the depth
   const unsigned band = tile / (4 * nw), in_band = tile - band * (4 * nw);
   const unsigned band_rows = nt - 4 * band < 4 ? nt - 4 * band : 4;
   const unsigned tw = in_band / band_rows, tt = 4 * band + (in_band - tw * band_rows);
-  const int64_t row0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(tt)) * TALL;
+  const int64_t row0 = first_row + static_cast<int64_t>(__builtin_amdgcn_readfirstlane(tt)) * TALL;
   const int64_t col0 = static_cast<int64_t>(__builtin_amdgcn_readfirstlane(tw)) * kCols;
 
   const int seg_steps = static_cast<int>((p.depth + kStep - 1) / kStep), steps = seg_steps * p.segments;
@@ -382,15 +386,37 @@ __global__ __launch_bounds__(512, 2) void wide_kernel(Product p, int splits) {
   }
 }
 
+template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED, int TALL>
+__global__ __launch_bounds__(512, 2) void wide_kernel(Product p, int splits) {
+  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes<TALL>];
+  wide_tile<ELEM, WIDE_STRIDED, TALL_STRIDED, GATED, TALL>(p, splits, lds, 0, p.rows, blockIdx.x, gridDim.x);
+}
+
+// Tiles of 256 rows of tall for the first `rows` of them, whose workgroups come first, and of 128 for the
+// rest.
+template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED>
+__global__ __launch_bounds__(512, 2) void mixed_kernel(Product p, int64_t rows, unsigned tiles) {
+  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes<256>];
+  static_assert(kLdsBytes<128> <= kLdsBytes<256>, "one allocation for both");
+  if (blockIdx.x < tiles)
+    wide_tile<ELEM, WIDE_STRIDED, TALL_STRIDED, GATED, 256>(p, 1, lds, 0, rows, blockIdx.x, tiles);
+  else
+    wide_tile<ELEM, WIDE_STRIDED, TALL_STRIDED, GATED, 128>(p, 1, lds, rows, p.rows - rows, blockIdx.x - tiles,
+                                                            gridDim.x - tiles);
+}
+
 // Adds the parts of a split product in order: one thread per four outputs.
 template <int ELEM, bool GATED>
 __global__ __launch_bounds__(256) void join_kernel(Product p, int splits) {
   using Acc = typename Elem<ELEM>::Acc;
-  const int64_t quads = (p.cols + 3) / 4, o = blockIdx.x * int64_t{256} + threadIdx.x;
-  if (o >= quads * p.rows * p.batch) return;
-  const int64_t line = o / quads, q = o - line * quads, ld = (GATED ? 2 : 1) * quads;      // rows of every output
-  const int z = static_cast<int>(line / p.rows);
-  const int64_t row = line - z * p.rows, stride = p.batch * p.rows * ld;
+  // A split product has fewer tiles than compute units: its outputs are counted in 32 bits.
+  const unsigned quads = static_cast<unsigned>((p.cols + 3) / 4), rows = static_cast<unsigned>(p.rows);
+  const unsigned o = blockIdx.x * 256u + threadIdx.x;
+  if (o >= quads * rows * p.batch) return;
+  const unsigned line = o / quads, q = o - line * quads;      // rows of every output
+  const int64_t ld = (GATED ? 2 : 1) * static_cast<int64_t>(quads), stride = p.batch * p.rows * ld;
+  const int z = p.batch > 1 ? static_cast<int>(line / rows) : 0;
+  const int64_t row = line - z * rows;
   const Acc* src = static_cast<const Acc*>(p.ws) + line * ld + q;
   Acc a = {}, b = {};
 #pragma unroll 4
@@ -399,9 +425,9 @@ __global__ __launch_bounds__(256) void join_kernel(Product p, int splits) {
     if (GATED) b += src[s * stride + quads];
   }
   WideScales<ELEM, GATED> sw;
-  sw.load(p, 4 * q);
+  sw.load(p, int64_t{4} * q);
   with_out_type<ELEM>(p, [&](auto type) {
-    finish4<ELEM, GATED, decltype(type)::value>(p, z, row, 4 * q, a, b, ELEM == kElemI8 ? p.tall_scale[row] : 1.0f, sw);
+    finish4<ELEM, GATED, decltype(type)::value>(p, z, row, int64_t{4} * q, a, b, ELEM == kElemI8 ? p.tall_scale[row] : 1.0f, sw);
   });
 }
 
@@ -417,8 +443,17 @@ void launch_tiles(const Product& p, int splits, hipStream_t stream) {
   }
 }
 
+template <int ELEM, bool WS, bool TS, bool GATED>
+void launch_mixed(const Product& p, int64_t rows, hipStream_t stream) {
+  const int64_t per = GATED ? 128 : 256, across = (p.cols + per - 1) / per * p.batch;
+  const int64_t tiles = across * (rows / 256), small = across * ((p.rows - rows + 127) / 128);
+  mixed_kernel<ELEM, WS, TS, GATED><<<dim3(static_cast<unsigned>(tiles + small)), 512, 0, stream>>>(
+      p, rows, static_cast<unsigned>(tiles));
+}
+
 template <int ELEM, bool WS, bool GATED>
 void launch_tall(const Product& p, const WidePlan& plan, hipStream_t stream) {
+  if (plan.mixed) return launch_mixed<ELEM, WS, false, GATED>(p, plan.mixed, stream);
   if (plan.tall == 64) launch_tiles<ELEM, WS, false, GATED, 64>(p, plan.splits, stream);
   else if (plan.tall == 128) launch_tiles<ELEM, WS, false, GATED, 128>(p, plan.splits, stream);
   else launch_tiles<ELEM, WS, false, GATED, 256>(p, plan.splits, stream);
@@ -428,6 +463,7 @@ template <int ELEM>
 void launch_elem(const Product& p, const WidePlan& plan, hipStream_t stream) {
   if (p.gated) return launch_tall<ELEM, false, true>(p, plan, stream);
   if constexpr (ELEM == kElemI8) launch_tall<ELEM, false, false>(p, plan, stream);
+  else if (p.tall_strided && plan.mixed) launch_mixed<ELEM, true, true, false>(p, plan.mixed, stream);
   else if (p.tall_strided && plan.tall == 128) launch_tiles<ELEM, true, true, false, 128>(p, plan.splits, stream);
   else if (p.tall_strided) launch_tiles<ELEM, true, true, false, 256>(p, plan.splits, stream);
   else launch_tall<ELEM, true, false>(p, plan, stream);
@@ -445,6 +481,7 @@ size_t wide_part_bytes(const Product& p, int splits) {
 //   a launch 2.5 us; a turn of the chip 2, 3.5 or 7.5 us for its first copies and its outputs and
 //   0.62, 0.72 or 1.1 us per step at 64, 128 or 256 rows of tall, up to 45 % more with every compute
 //   unit at work (power), or what the turn's rows of wide take from memory at 5 TB/s;
+//   a tile of 128 rows 0.57 of one of 256;
 //   the partial sums 2.5 us and their bytes, written and read, at 6 TB/s.
 WidePlan wide_plan(const Product& p) {
   const int64_t bytes = p.elem == kElemI8 ? 1 : 2, units = device_compute_units();
@@ -458,13 +495,17 @@ WidePlan wide_plan(const Product& p) {
       const int64_t at_once = std::min(tiles * splits, units), turns = (tiles * splits + units - 1) / units;
       const double busy = static_cast<double>(at_once) / units;
       const double memory = std::min(col_tiles * splits, at_once) * 32768.0 / 5e6;
-      double us = 2.5 + turns * (ends + (steps + splits - 1) / splits * std::max(step * (1 + 0.45 * busy), memory));
+      const double turn = ends + (steps + splits - 1) / splits * std::max(step * (1 + 0.45 * busy), memory);
+      double us = 2.5 + turns * turn;
       if (splits > 1) us += 2.5 + wide_part_bytes(p, splits) * 2 / 6e6;
-      if (best.splits == 0 || us < best.us) {
-        best.tall = tall;
-        best.splits = splits;
-        best.us = us;
-      }
+      if (best.splits == 0 || us < best.us) best = {tall, splits, 0, us};
+      // Whole turns of 256 rows, the rest in tiles of 128 that fill one more.
+      const int64_t first = tiles / units * units / col_tiles, rest = p.rows - 256 * first;
+      if (tall != 256 || splits > 1 || first == 0 || rest <= 0) continue;
+      const int64_t early = tiles / units * units - first * col_tiles;      // workgroups done a turn before
+      const int64_t small = col_tiles * ((rest + 127) / 128) - early * 7 / 4;
+      us = 2.5 + turn * (tiles / units + 0.57 * std::max<int64_t>((small + units - 1) / units, 0));
+      if (us < best.us) best = {tall, splits, 256 * first, us};
     }
   }
   return best;

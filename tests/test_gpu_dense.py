@@ -13,7 +13,7 @@ F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
 SIZES = [(1, 1, 1), (1, 5, 3), (1, 64, 64), (1, 130, 2048), (2, 64, 130), (3, 129, 77), (5, 48, 1000), (8, 256, 512),
          (12, 100, 264), (16, 33, 1001), (17, 96, 72), (33, 520, 136), (64, 200, 1024), (65, 31, 513), (100, 300, 999),
          (128, 128, 192), (257, 136, 320), (300, 700, 640), (520, 513, 257)]
-LARGE = [(600, 1088, 768), (1025, 520, 1096), (2100, 264, 512)]
+LARGE = [(600, 1088, 768), (1025, 520, 1096), (2100, 264, 512), (4000, 4500, 72)]
 
 
 def _guarded(shape, dtype):
