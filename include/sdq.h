@@ -397,7 +397,8 @@ sdq_status sdq_linear_expanded(int64_t m, const void* codes_dev, const float* sc
  * Nothing is allocated, synchronised or kept, so every call can be captured
  * in a graph; calls that share a workspace must be ordered (same stream).
  * Results are bitwise deterministic.  Sizes whose tiles do not fit one launch
- * (about 1.7e10 outputs) return SDQ_ERR_SHAPE.
+ * (8e9 outputs), and rows of 2^22 or more elements of a
+ * dense block, return SDQ_ERR_SHAPE.
  */
 
 /* act(g) of the gated block: g / (1 + e^-g), or GELU in its tanh form. */

@@ -9,6 +9,13 @@ namespace sdq {
 // Element types of an operand as the kernels are instantiated.
 enum ElemType { kElemF16 = SDQ_F16, kElemBf16 = SDQ_BF16, kElemI8 = 3 };
 
+// How a product is cut on tiles (dense_wide.hip): rows of tall to a tile and the parts of the depth.
+struct WidePlan {
+  int tall = 256, splits = 0;
+  int64_t mixed = 0;                  // tiles of 256 rows for so many of them, of 128 for the rest
+  double us = 0;                      // about what it takes
+};
+
 // One matrix product of the dense operators,
 //   out[i][r] = sum_c wide(r, c) tall(i, c),   i < rows, r < cols, c < depth,
 // with r the contiguous dimension of the output.  An operand is stored with c
@@ -45,9 +52,14 @@ struct Product {
   void* u_out = nullptr;
   // product_ws_bytes of workspace
   void* ws = nullptr;
+  // The kernel, by plan_product from the sizes, the operands' rows and flags.
+  bool few = false;
+  WidePlan plan;
 };
 
-// The workspace that launch_product needs for this product (pointers not read): copies of
+void plan_product(Product* p);
+
+// The workspace that launch_product needs for this planned product (pointers not read): copies of
 // operands whose rows do not start 16-byte aligned, partial sums.
 size_t product_ws_bytes(const Product& p);
 // The elements from row to row with which the product takes an operand of n-element rows as it
@@ -62,16 +74,11 @@ bool product_quantizes(const Product& p);
 void launch_few(const Product& p, hipStream_t stream);
 bool few_quantizes(const Product& p);
 double few_us(const Product& p);      // about what it takes
-// Tiles of 256 rows of wide, rows aligned (dense_wide.hip): how many rows of tall to a tile, and into
-// how many parts the depth is cut, whose sums take wide_part_bytes of the workspace.
-struct WidePlan {
-  int tall = 256, splits = 0;
-  int64_t mixed = 0;                  // tiles of 256 rows for so many of them, of 128 for the rest
-  double us = 0;                      // about what it takes
-};
+// Tiles of 256 rows of wide, rows aligned (dense_wide.hip); the sums of a depth in parts take
+// wide_part_bytes of the workspace.
 WidePlan wide_plan(const Product& p);
 size_t wide_part_bytes(const Product& p, int splits);
-void launch_wide(const Product& p, const WidePlan& plan, hipStream_t stream);
+void launch_wide(const Product& p, hipStream_t stream);
 
 // Codes in rows of ld, those past k zeros.
 sdq_status launch_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, int8_t* q, int64_t ld,

@@ -16,7 +16,7 @@ bool known_act(int32_t act) { return act == SDQ_ACT_SILU || act == SDQ_ACT_GELU_
 constexpr int64_t kMaxRows = int64_t{1} << 29;
 constexpr int64_t kMaxRowLength = (int64_t{1} << 22) - 16;   // 256 rows of 16-bit elements are addressed with 31 bits
 constexpr int64_t kMaxInt8Depth = 131071;         // 128 * 128 * k stays below 2^31
-constexpr int64_t kMaxTiles = int64_t{1} << 23;   // of 32 x 64 outputs: threads of one launch fit 32 bits
+constexpr int64_t kMaxTiles = int64_t{1} << 22;   // of 32 x 64 outputs: threads of one launch fit 32 bits
 
 sdq_status check_sizes(int64_t m, int64_t n, int64_t k, bool int8) {
   if (m < 0 || n < 0 || k <= 0)
@@ -58,6 +58,7 @@ Product int8_product(int64_t m, int64_t n, int64_t k, bool gated) {
   p.cols = n;
   p.depth = p.ld_wide = p.ld_tall = k;
   p.gated = gated;
+  plan_product(&p);
   return p;
 }
 
@@ -116,6 +117,7 @@ Product gated_product(sdq_dtype t, int64_t m, int64_t f, int64_t k) {
   p.depth = p.ld_wide = p.ld_tall = k;
   p.gated = true;
   p.out_type = t;
+  plan_product(&p);
   return p;
 }
 
@@ -131,6 +133,7 @@ Product input_gradient(sdq_dtype t, int64_t m, int64_t f, int64_t k) {
   p.segments = 2;
   p.out_type = t;
   p.ld_tall = product_ld(p, f);
+  plan_product(&p);
   return p;
 }
 
@@ -146,6 +149,7 @@ Product weight_gradient(sdq_dtype t, int64_t m, int64_t f, int64_t k) {
   p.batch = 2;
   p.out_type = t;
   p.ld_tall = product_ld(p, f);
+  plan_product(&p);
   return p;
 }
 
@@ -176,7 +180,7 @@ sdq_status sdq_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, 
                              void* stream) {
   if (!float_type(xt)) return set_error(SDQ_ERR_ARG, "bad dtype");
   if (m < 0 || k <= 0) return set_error(SDQ_ERR_ARG, "need m >= 0 and k > 0");
-  if (m > kMaxTiles || k > kMaxRows) return set_error(SDQ_ERR_SHAPE, "m=%lld k=%lld is too large for one launch",
+  if (m > kMaxRows || k > kMaxRows) return set_error(SDQ_ERR_SHAPE, "m=%lld k=%lld is too large for one launch",
                                                       (long long)m, (long long)k);
   if (m == 0) return SDQ_OK;
   if (!x || !q || !scales) return set_error(SDQ_ERR_ARG, "NULL pointer argument");

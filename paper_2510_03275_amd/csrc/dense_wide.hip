@@ -491,7 +491,7 @@ WidePlan wide_plan(const Product& p) {
   for (int tall = 256; tall >= (p.tall_strided ? 128 : 64); tall /= 2) {
     const int64_t tiles = col_tiles * ((p.rows + tall - 1) / tall);
     const double step = tall == 256 ? 1.1 : tall == 128 ? 0.72 : 0.62, ends = tall == 256 ? 7.5 : tall == 128 ? 3.5 : 2.0;
-    for (int splits = 1; splits <= 32 && (splits == 1 || steps / splits >= 3); ++splits) {
+    for (int splits = 1; splits <= 32 && (splits == 1 || (steps / splits >= 3 && tiles * splits <= 3 * units)); ++splits) {
       const int64_t at_once = std::min(tiles * splits, units), turns = (tiles * splits + units - 1) / units;
       const double busy = static_cast<double>(at_once) / units;
       const double memory = std::min(col_tiles * splits, at_once) * 32768.0 / 5e6;
@@ -511,10 +511,10 @@ WidePlan wide_plan(const Product& p) {
   return best;
 }
 
-void launch_wide(const Product& p, const WidePlan& plan, hipStream_t stream) {
-  if (p.elem == kElemF16) launch_elem<kElemF16>(p, plan, stream);
-  else if (p.elem == kElemBf16) launch_elem<kElemBf16>(p, plan, stream);
-  else launch_elem<kElemI8>(p, plan, stream);
+void launch_wide(const Product& p, hipStream_t stream) {
+  if (p.elem == kElemF16) launch_elem<kElemF16>(p, p.plan, stream);
+  else if (p.elem == kElemBf16) launch_elem<kElemBf16>(p, p.plan, stream);
+  else launch_elem<kElemI8>(p, p.plan, stream);
 }
 
 }  // namespace sdq

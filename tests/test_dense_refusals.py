@@ -110,3 +110,36 @@ def test_plain_quantiser():
     q, s = D.quantize_ref(x)
     assert q[0].tolist() == [0, 2, 2, 0, -2, 127] and float(s[0]) == 1.0
     assert not q[1].any() and float(s[1]) == 2.0 ** -126 and not q[2].any() and math.isnan(float(s[2]))
+
+
+def test_native_and_ctypes_calls_answer_alike(monkeypatch):
+    """The native calls of the per-token entry points and the ctypes ones that stand in for them."""
+    import sys
+    import types
+    stream = types.SimpleNamespace(cuda_stream=0)
+    x, w, s = torch.zeros(2, 8, dtype=torch.bfloat16), torch.zeros(4, 8, dtype=torch.int8), torch.zeros(4)
+    names = ("_call_int8_linear", "_call_int8_gated_linear", "_call_gated_linear")
+    native = [getattr(Bd, n) for n in names]
+    monkeypatch.setitem(sys.modules, "paper_2510_03275_amd._sdqcall", None)
+    monkeypatch.delattr(P, "_sdqcall", raising=False)
+    plain = Bd._native_dense_calls()
+    seen = []
+    for calls in (native, plain):
+        for n, c in zip(names, calls):
+            monkeypatch.setattr(Bd, n, c)
+        got = []
+        for fn in (lambda: P.sdq_int8_linear(x, w, s, torch.zeros(2, 4), None, stream),      # 2 rows of 8: no workspace
+                   lambda: P.sdq_int8_linear(x.new_zeros(0, 8), w, s, torch.zeros(0, 4), None, stream),
+                   lambda: P.sdq_int8_gated_linear(x, w, s, w, s, 5, x, x, stream),
+                   lambda: P.sdq_int8_gated_linear(torch.zeros(99, 600), w.new_zeros(4, 600), s, w.new_zeros(4, 600), s, 0,
+                                                   x, x, stream),
+                   lambda: P.sdq_gated_linear(x, x, x, 7, x, x, stream),
+                   lambda: P.sdq_gated_linear(x, x, x, 0, x, x, stream, g=x)):
+            try:
+                fn()
+                got.append(0)
+            except P.SdqError as e:
+                got.append((e.status, str(e)))
+        seen.append(got)
+    assert seen[0] == seen[1]
+    assert [g if g == 0 else g[0] for g in seen[0]] == [WORKSPACE, 0, ARG, WORKSPACE, ARG, ARG]

@@ -13,7 +13,8 @@ F16, BF16, F32 = torch.float16, torch.bfloat16, torch.float32
 SIZES = [(1, 1, 1), (1, 5, 3), (1, 64, 64), (1, 130, 2048), (2, 64, 130), (3, 129, 77), (5, 48, 1000), (8, 256, 512),
          (12, 100, 264), (16, 33, 1001), (17, 96, 72), (33, 520, 136), (64, 200, 1024), (65, 31, 513), (100, 300, 999),
          (128, 128, 192), (257, 136, 320), (300, 700, 640), (520, 513, 257)]
-LARGE = [(600, 1088, 768), (1025, 520, 1096), (2100, 264, 512), (4000, 4500, 72)]
+# several tiles in every direction; more tiles than compute units in h, in the gradients of the weights, in dx
+LARGE = [(600, 1088, 768), (1025, 520, 1096), (2100, 264, 512), (4000, 4500, 72), (40, 6000, 1800), (6100, 40, 3400)]
 
 
 def _guarded(shape, dtype):
@@ -73,7 +74,11 @@ def test_quantize_special_rows(dtype):
     assert torch.equal(torch.isnan(r.scales.cpu()), torch.isnan(ref_s))
     assert torch.equal(torch.nan_to_num(r.scales.cpu()), torch.nan_to_num(ref_s))
     assert torch.equal(r.q.cpu().long(), ref_q)
-    y = P.int8_linear(x.cuda(), _rows8(P, *_codes(1, 40, k)), dtype=F32)
+    w = _rows8(P, *_codes(1, 40, k))
+    y = P.int8_linear(x.cuda(), w, dtype=F32)
+    for i in range(12):      # one row: quantised by the product itself
+        one = P.int8_linear(x[i:i + 1].cuda(), w, dtype=F32)
+        assert torch.equal(one.nan_to_num(7), y[i:i + 1].nan_to_num(7)), i
     assert torch.equal(torch.isnan(y).all(1).cpu(), torch.isnan(ref_s))
     assert not bool(torch.isnan(y[:5]).any())
 
@@ -285,6 +290,80 @@ def test_graph_replays_match_eager(m, f, k):
             assert all(torch.equal(a, b) for a, b in zip(out, want)), rep
             assert all(torch.equal(a, b) for a, b in zip(s(), want)), rep
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("m", [1, 30, 300])
+def test_graphs_share_a_workspace(m):
+    """Two graphs captured on one workspace, replayed in turn on one stream, with eager calls on it between."""
+    require_gpu()
+    import paper_2510_03275_amd as P
+    f, k = 520, 264
+    ws = torch.empty(max(P.sdq_int8_gated_linear_workspace_bytes(m, f, k),
+                         P.sdq_gated_linear_backward_workspace_bytes(m, f, k)), dtype=torch.uint8, device="cuda")
+    wg, wu = (D.rand(i, f, k, scale=k ** -0.5).to(BF16).cuda() for i in (2, 3))
+    g8, u8 = P.int8_quantize(wg), P.int8_quantize(wu)
+    x, dh = D.rand(1, m, k).to(BF16).cuda(), D.rand(4, m, f).to(BF16).cuda()
+    g, u = (D.rand(i, m, f).to(BF16).cuda() for i in (5, 6))
+    first = lambda: [P.int8_gated_linear(x, g8, u8, workspace=ws), P.gated_linear(x, wg, wu, workspace=ws)]
+    second = lambda: list(P.gated_linear_backward(dh, x, wg, wu, g, u, workspace=ws))
+    want = [[v.clone() for v in c()] for c in (first, second)]
+    graphs = []
+    for call in (first, second):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = call()
+        graphs.append((graph, out))
+    for rep in range(3):
+        for (graph, out), w, call in zip(graphs, want, (second, first)):
+            for o in out:
+                o.fill_(float("nan"))
+            ws.fill_(255)
+            graph.replay()
+            call()
+            torch.cuda.synchronize()
+            assert all(torch.equal(a, b) for a, b in zip(out, w)), rep
+
+
+def test_beyond_two_to_the_31_elements():
+    """h, its gradient and the block's own of 2.2e9 elements each: the last rows and columns come out right."""
+    require_gpu()
+    import paper_2510_03275_amd as P
+    m, f, k = 66000, 33000, 64
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    x = torch.randn(m, k, generator=gen, device="cuda", dtype=BF16)
+    wg, wu = (torch.randn(f, k, generator=gen, device="cuda", dtype=BF16) * 0.125 for _ in range(2))
+    g, u = (torch.empty(m, f, dtype=BF16, device="cuda") for _ in range(2))
+    h = P.gated_linear(x, wg, wu, g=g, u=u)
+    rows, cols = [0, 32600, m - 1], [0, 17000, f - 1]
+    gr, ur, eg, eu = D.gated_ref(x[rows].cpu(), wg.cpu(), wu.cpu(), 0)
+    D.assert_close(h[rows], *D.gated_bound(gr, ur, eg, eu, 0, BF16))
+    dh = torch.randn(m, f, generator=gen, device="cuda", dtype=BF16)
+    dx, dg, du = P.gated_linear_backward(dh, x, wg, wu, g, u)
+    ref = D.backward_ref(dh[rows].cpu(), x[rows].cpu(), wg.cpu(), wu.cpu(), g[rows].cpu(), u[rows].cpu(), 0, BF16)
+    D.assert_close(dx[rows], *ref[0], "dx")
+    # the gradients of some rows of the weights: sums over every token
+    ref = D.backward_ref(dh[:, cols].cpu(), x.cpu(), wg[cols].cpu(), wu[cols].cpu(), g[:, cols].cpu(), u[:, cols].cpu(),
+                         0, BF16)
+    D.assert_close(dg[cols], *ref[1], "dgate")
+    D.assert_close(du[cols], *ref[2], "dup")
+    del dh, dx, dg, du, g, u
+    # the same rows through 8 bits, against the product of the last ones alone
+    w8 = P.int8_quantize(wg)
+    y = P.int8_linear(x, w8, out=h)
+    last = P.int8_linear(x[m - 200:].contiguous(), w8)
+    assert torch.equal(y[m - 200:], last)
+
+
+def test_rows_beyond_two_to_the_20():
+    """More rows than one launch has workgroups."""
+    require_gpu()
+    import paper_2510_03275_amd as P
+    m = (1 << 20) + 300
+    for k in (3, 1100):       # a wave and a workgroup to a row
+        x = torch.randn(m if k > 100 else 4 * m, k, device="cuda", dtype=F16)
+        r = P.int8_quantize(x)
+        part = P.int8_quantize(x[-500:].clone())      # a copy starts aligned
+        assert torch.equal(r.q[-500:], part.q) and torch.equal(r.scales[-500:], part.scales)
 
 
 @pytest.mark.parametrize("m", [3, 90])
