@@ -302,32 +302,32 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
     }
   };
 
-  // Copies newer than a step's, of which the last stages are filled in the order of the steps: where
-  // tall has fewer stages than wide, the newest step of wide.
+  // Copies newer than a step's when it is waited for: wide is copied in a step's first half and tall in
+  // its second.
   constexpr int kNewer = kTallStages < kWideStages ? kWideCopies : (kTallStages - 2) * (kTallCopies + kWideCopies);
-  typedef std::integral_constant<int, 0> NoCopies;
-  typedef std::integral_constant<int, kTallCopies + kWideCopies> Copies;
+  typedef std::integral_constant<int, kTallCopies> TallCopies;
+  typedef std::integral_constant<int, kWideCopies> WideCopies;
   typedef std::integral_constant<int, kNewer> Newer;
-  typedef std::integral_constant<int, kNewer + kTallCopies + kWideCopies> First;
+  typedef std::integral_constant<int, (kTallStages - 1) * kTallCopies + (kWideStages - 2) * kWideCopies> First;
 #pragma unroll
   for (int s = 0; s < kWideStages; ++s) {
     if (s < kTallStages) copy_a(t0 + s, std::true_type());
-    copy_b(t0 + s, std::true_type());
+    if (s < kWideStages - 1) copy_b(t0 + s, std::true_type());
   }
   turn(First());
   read(0);
   auto step = [&](int t, auto mask) {
+    copy_b(t + kWideStages - 1, mask);      // to the stage of step t - 1
     read(1);
     multiply(0);
-    spread(NoCopies());
+    spread(WideCopies());
     turn(Newer());              // step t is in registers, step t + 1 in LDS
-    copy_a(t + kTallStages, mask);
-    copy_b(t + kWideStages, mask);
+    copy_a(t + kTallStages, mask);          // to the stage of step t
     get_a = next_a(get_a);
     get_b = next_b(get_b);
     read(0);
     multiply(1);
-    spread(Copies());
+    spread(TallCopies());
     __builtin_amdgcn_sched_barrier(0);
   };
   // Steps that no copy has to be masked for: all but a segment's last.
