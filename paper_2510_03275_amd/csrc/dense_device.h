@@ -67,8 +67,9 @@ __device__ inline void act_both(float g, int act, float* value, float* slope) {
   *slope = e > 0.0f && s > 0.0f ? s + g * s * (e * s) * da : s;
 }
 
-// Four consecutive outputs r .. r + 3 of row i (those below cols) of type TYPE; vector
-// stores where the row length keeps every group of four aligned.
+// Four consecutive outputs r .. r + 3 of row i (those below cols) of type TYPE.  Rows need not start
+// aligned: the memory takes a vector at any address (stored one by one, the odd rows of 777 x 2731
+// cost more than their product).
 template <int TYPE> struct Out;
 template <> struct Out<SDQ_F16> { using Scalar = _Float16; using Four = f16x4; };
 template <> struct Out<SDQ_BF16> { using Scalar = __bf16; using Four = bf16x4; };
@@ -78,10 +79,14 @@ __device__ inline void store4(void* out, int64_t i, int64_t r, int64_t cols, boo
   using S = typename Out<TYPE>::Scalar;
   using F = typename Out<TYPE>::Four;
   S* at = static_cast<S*>(out) + i * cols + r;
-  if (cols % 4 == 0) {
-    F* p = reinterpret_cast<F*>(at);
-    if (accumulate) v += __builtin_convertvector(*p, f32x4);
-    *p = __builtin_convertvector(v, F);
+  if (r + 4 <= cols) {
+    F f;
+    if (accumulate) {
+      __builtin_memcpy(&f, at, sizeof(F));
+      v += __builtin_convertvector(f, f32x4);
+    }
+    f = __builtin_convertvector(v, F);
+    __builtin_memcpy(at, &f, sizeof(F));
     return;
   }
 #pragma unroll

@@ -265,12 +265,12 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
   Acc acc[kFrags][4] = {};        // [rows of tall / 16][rows of wide / 16]
   i32x4 a[2][kFrags], b[2][4];    // [depth half][rows / 16]
   auto read = [&](int s) {
+    // In the order in which the products ask for them.
+    a[s][0] = fa.read(lds + get_a, 0, s);
 #pragma unroll
-    for (int n = 0; n < (kFrags > 4 ? kFrags : 4); ++n) {
-      if (n < kFrags) a[s][n] = fa.read(lds + get_a, n, s);
-      if (kFrags <= 4) b[s][n] = fb.read(lds + get_b, n, s);
-      else if (n % 2) b[s][n / 2] = fb.read(lds + get_b, n / 2, s);
-    }
+    for (int n = 0; n < 4; ++n) b[s][n] = fb.read(lds + get_b, n, s);
+#pragma unroll
+    for (int n = 1; n < kFrags; ++n) a[s][n] = fa.read(lds + get_a, n, s);
   };
   auto multiply = [&](int s) {
 #pragma unroll
