@@ -9,6 +9,8 @@
  * first-order Sigma-Delta scan) and evaluates y = x W_hat^T directly on the
  * codes (Fig. 5: the activations are expanded to the oversampled length and
  * contracted against the codes, additions only in the decode kernel).
+ * Beside them stand layers that a model keeps dense: products in 8-bit
+ * integers, and the gated feed-forward block with its gradients.
  *
  * Conventions for every entry point:
  *  - Pointers named *_dev are device (HBM) pointers, *_host are host pointers.

@@ -1,6 +1,7 @@
 """SDQ-LLM hot path on MI355X: Sigma-Delta weight encoder and addition-only
 linear layer as hand-written HIP kernels for gfx950 behind a C ABI
-(include/sdq.h).  This package is the thin Python binding of that library."""
+(include/sdq.h), with 8-bit linears and the gated feed-forward block beside them.
+This package is the thin Python binding of that library."""
 from .binding import (  # noqa: F401
     Encoded, SdqError, lib, linear, quantize, sdq_codes_bytes, sdq_compression_ratio, sdq_layout,
     sdq_layout_init, sdq_layout_set_hadamard, sdq_layout_set_packing, sdq_linear, sdq_expand_activations,

@@ -1,16 +1,16 @@
-// The products of the dense operators for at most 64 rows (token generation):
-// the weights are read once and everything else is small, so the stream of the
-// weights bounds it.
+// The products of the dense operators for at most 64 rows (token generation),
+// where the stream of the weights bounds them: one row of bf16 against gate and up of
+// 11008 x 4096 (180 MB) in 31.5 us, 5.7 TB/s; of 8 bits against 8192 x 28672 in 36 us, 6.5 TB/s.
 //
-// A workgroup forms 16 rows of wide for each of its TILES (of a gated product,
-// half of them gate and the other half the same columns of up) times 16 TALL rows, its waves each a contiguous part of the
-// depth; their sums are joined through LDS as a fixed tree, so results do
-// not depend on timing and need no second launch.  A wave reads its weights from memory into
-// the matrix-core operand registers (lane l: row l % 16, 16 bytes at l / 16 of a
-// 64-byte step), some steps ahead of the products; the activations come from L2
-// the same way, rows past the last as copies of it whose outputs are not
-// stored.  Rows need not start aligned: only the bytes behind the last whole
-// step are read element by element.
+// A workgroup forms 16 rows of wide for each of its TILES (of a gated product, half of
+// them gate and the other half the same columns of up) times 16 TALL rows, its waves
+// each a contiguous part of the depth; their sums are joined through LDS as a fixed
+// tree, so results do not depend on timing and need no second launch.  A wave reads
+// its weights from memory into the matrix-core operand registers (lane l: row l % 16,
+// 16 bytes at l / 16 of a 64-byte step), two steps ahead of the products; the
+// activations come from L2 the same way, rows past the last as copies of it whose
+// outputs are not stored.  Rows need not start aligned: only the bytes behind the last
+// whole step are read element by element.
 //
 // A small call on 8-bit weights quantises its rows itself: every workgroup forms the codes of all rows
 // in LDS while its first weights are on their way, which saves the launch of

@@ -1,41 +1,43 @@
 // The products of the dense operators on tiles of 256 rows of wide by 256, 128
 // or 64 rows of tall (dense.h), for operands whose rows start 16-byte aligned.
 //
-// What bounds it, at 256 x 256: a step of 128 bytes of depth takes 64 matrix-core
-// instructions per wave (two waves per SIMD: 2048 clocks per step), 192 KB of LDS
-// reads (1536 clocks at 128 bytes) and 64 KB of copies into LDS.  So the
-// matrix cores and LDS have to run side by side, and nothing may wait for memory:
+// What bounds it, at 256 x 256: a step of 128 bytes of depth keeps the matrix
+// cores of a SIMD for 2048 clocks; beside it go 192 KB of LDS reads (768 clocks), 64 KB
+// of copies from L2 and the waits of a barrier.  Measured on bf16 2048 x (2 x 28672) x 8192:
+// the matrix cores work 80 % of 2.3 M clocks, no LDS bank conflicts, and random data
+// brings the clock down to 1.78 GHz (power), so what an instruction costs in energy counts
+// as much as what it hides: 1.35-1.42 PFLOP/s fused with its activation, where a library's plain
+// product of the same size reaches 1.41-1.46 on the same boxes; 8-bit 4096 x 28672 x 8192
+// 2.5-2.7 POP/s (library 2.3).
 //
-//   tile      Eight waves; wave (wt, ww) multiplies rows 64 wt .. of both 128-row
-//             halves of tall (A0, A1) with rows 32 ww .. of both halves of wide
-//             (B0, B1): 128 x 64 outputs in 128 registers.  Of a gated product B0 is
-//             gate and B1 the same 128 rows of up, so a lane ends with g and u of
-//             the same outputs.
-//   phases    A step is four phases: read A0, multiply A0 B0; read B1, A0 B1; read
-//             A1, A1 B0; read the next step's B0, A1 B1.  Each phase is a reading
-//             part, a barrier, 16 matrix-core instructions, a barrier.  Waves 4-7
-//             run half a phase behind waves 0-3 (one barrier more before, one less
-//             after), so one half of the workgroup reads LDS while the other
-//             multiplies.
-//   copies    Two steps sit in LDS.  A quarter (A0, A1, B0 or B1, 16 KB) is read in
-//             one phase and refilled with the step after next in the phase that
-//             follows: straight from memory to LDS, two 1 KB copies per wave.
-//             Every phase ends with a wait for all but the last 12 copies, which
-//             is the quarter read next: copies have six phases to arrive.
+//   tile      Eight waves, two to a SIMD; wave (wt, ww) forms half the rows of tall by
+//             64 of wide with 16 x 16 matrix instructions (128 x 64 in 128 registers).  (Four waves of
+//             128 x 128 on 32 x 32 instructions: 11 % slower, and twice the accumulator traffic.)  Of a
+//             gated product the tile's rows of wide are 128 of gate and the same 128 of up.
+//   steps     The operands of half a step (64 bytes of depth) are read from LDS while the other
+//             half is multiplied, in the order in which the products ask for them; one barrier a step.
+//             (Reading and multiplying by turns in two halves of the workgroup: 6 % slower.)
+//   copies    go straight from memory to LDS, the next steps' stage by stage (160 KB of stages, Stages
+//             below): wide's in a step's first half, tall's in its second.  A step waits for all
+//             copies but the newest ones (kNewer), counted, before its barrier; the barrier ends the
+//             reads of the stage that is filled next.  A step takes whole 128-byte lines: in steps
+//             of 64 bytes, L2 served twice the requests (operands of zeros, which no power limit
+//             holds back: 1490 against 1760 TFLOP/s).
 //   layout    Depth-contiguous operands: LDS rows of 128 bytes whose 16-byte chunk q
 //             lies at q ^ (row % 8) (the copy permutes its source addresses; LDS
-//             addresses of a copy are linear), so that eight lanes' reads of eight
-//             rows cover all banks.  Strided operands: LDS rows of one depth (128
+//             addresses of a copy are linear): no conflicts among the 16 lanes that are served at once.
+//             Strided operands: LDS rows of one depth (128
 //             elements); a group of 16 lanes reads 4 depths x 16 elements
 //             transposed (ds_read_b64_tr_b16), 32-byte granule p of depth c at
-//             p ^ (c % 4 + 4 (c / 8 % 2)).
-//   outputs   The sums go through LDS, half a tile at a time, so that the stores are
+//             p ^ (2 (c % 4) + c / 8 % 2).  So the gradients need no transposed copies in memory.
+//   outputs   The sums go through LDS, up to 128 rows at a time, so that the stores are
 //             whole rows and the code that scales, activates and converts exists once
 //             (unrolled over a lane's 128 sums it was 130 KB of instructions, whose
 //             first fetch took 20 us).
 //   splits    Where the tiles are fewer than the compute units, the depth is cut and
 //             the sums of every part go to the workspace; join_kernel adds them in
-//             order.
+//             order.  Where they are a turn of the chip and a part of one, the last rows
+//             go in tiles of 128 (mixed_kernel).
 //   ends      Buffer resources end with the operand: rows past its end read as
 //             zeros, as do depths past its end (for depth-contiguous rows, whose
 //             neighbours follow, the lanes past the end get an address out of range).
