@@ -396,6 +396,7 @@ sdq_status sdq_linear_expanded(int64_t m, const void* codes_dev, const float* sc
  * one column on; rows need not start aligned, matrices and workspaces start
  * 16-byte aligned (else SDQ_ERR_ARG).  m = 0 or n = 0 is a no-op.  Inputs may
  * hold any values: NaN and infinities go through the formulas of their rows.
+ * Outputs and workspaces overlap neither each other nor an input.
  * Nothing is allocated, synchronised or kept, so every call can be captured
  * in a graph; calls that share a workspace must be ordered (same stream).
  * Results are bitwise deterministic.  Sizes whose tiles do not fit one launch
@@ -455,8 +456,9 @@ sdq_status sdq_int8_gated_linear(const void* x_dev, sdq_dtype xt, const float* x
  * h = act(g) * u with g = x gate^T, u = x up^T, all of one type t (F16 or BF16;
  * SDQ_ERR_UNSUPPORTED for F32): x [m x k], gate and up [f x k], h [m x f].
  * Sums, g, u and the activation are fp32; h is rounded once.
- *   g_dev, u_dev   both NULL, or [m x f] each: g and u rounded to t, for
- *                sdq_gated_linear_backward.
+ *   g_dev, u_dev   both NULL (kt is not read then), or [m x f] each: g and u
+ *                for sdq_gated_linear_backward, of type kt: t (rounded), or F32
+ *                (as summed: gradients nearer by 1.3 to 1.8 times, twice the memory).
  *   workspace    >= sdq_gated_linear_workspace_bytes(m, f, k) bytes (may be
  *                NULL where that is 0), no initialisation needed.
  * Errors: SDQ_ERR_ARG, SDQ_ERR_SHAPE, SDQ_ERR_UNSUPPORTED, SDQ_ERR_WORKSPACE,
@@ -465,13 +467,13 @@ sdq_status sdq_int8_gated_linear(const void* x_dev, sdq_dtype xt, const float* x
 size_t sdq_gated_linear_workspace_bytes(int64_t m, int64_t f, int64_t k);
 sdq_status sdq_gated_linear(const void* x_dev, sdq_dtype t, int64_t m, const void* gate_dev, const void* up_dev,
                             int64_t f, int64_t k, int32_t act, void* h_dev, void* g_dev, void* u_dev,
-                            void* workspace_dev, size_t workspace_bytes, void* stream);
+                            sdq_dtype kt, void* workspace_dev, size_t workspace_bytes, void* stream);
 
 /*
  * Gradients of the gated block for dh (the gradient of h, [m x f] of type t):
  *   dg = dh * u * act'(g),  du = dh * act(g)      in fp32, rounded to t,
  *   dx = dg gate + du up,   dgate = dg^T x,   dup = du^T x     (fp32 sums),
- * with g and u as sdq_gated_linear wrote them.
+ * with g and u as sdq_gated_linear wrote them, of the same kt.
  *   dx_dev       [m x k], or NULL where it is not wanted.
  *   dgate_dev, dup_dev   [f x k] each, or both NULL (frozen weights; x is not
  *                read then).  accumulate nonzero: added into them (gradients
@@ -484,8 +486,8 @@ sdq_status sdq_gated_linear(const void* x_dev, sdq_dtype t, int64_t m, const voi
 size_t sdq_gated_linear_backward_workspace_bytes(int64_t m, int64_t f, int64_t k);
 sdq_status sdq_gated_linear_backward(const void* dh_dev, const void* x_dev, sdq_dtype t, int64_t m,
                                      const void* gate_dev, const void* up_dev, int64_t f, int64_t k, int32_t act,
-                                     const void* g_dev, const void* u_dev, void* dx_dev, void* dgate_dev,
-                                     void* dup_dev, int32_t accumulate, void* workspace_dev,
+                                     const void* g_dev, const void* u_dev, sdq_dtype kt, void* dx_dev,
+                                     void* dgate_dev, void* dup_dev, int32_t accumulate, void* workspace_dev,
                                      size_t workspace_bytes, void* stream);
 
 /*

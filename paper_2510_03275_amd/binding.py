@@ -118,11 +118,11 @@ def _load() -> ctypes.CDLL:
                                                  ctypes.c_size_t, P]),
         "sdq_gated_linear_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 3),
         "sdq_gated_linear": (ctypes.c_int, [P, ctypes.c_int, ctypes.c_int64, P, P, ctypes.c_int64, ctypes.c_int64,
-                                            ctypes.c_int32, P, P, P, P, ctypes.c_size_t, P]),
+                                            ctypes.c_int32, P, P, P, ctypes.c_int, P, ctypes.c_size_t, P]),
         "sdq_gated_linear_backward_workspace_bytes": (ctypes.c_size_t, [ctypes.c_int64] * 3),
         "sdq_gated_linear_backward": (ctypes.c_int, [P, P, ctypes.c_int, ctypes.c_int64, P, P, ctypes.c_int64,
-                                                     ctypes.c_int64, ctypes.c_int32, P, P, P, P, P, ctypes.c_int32,
-                                                     P, ctypes.c_size_t, P]),
+                                                     ctypes.c_int64, ctypes.c_int32, P, P, ctypes.c_int, P, P, P,
+                                                     ctypes.c_int32, P, ctypes.c_size_t, P]),
         "sdq_unpack_codes": (ctypes.c_int, [L, P, P]),
         "sdq_upsample_table": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32, P]),
         "sdq_prepare": (ctypes.c_int, [ctypes.c_int32, ctypes.c_int32]),
@@ -429,11 +429,13 @@ def sdq_gated_linear_workspace_bytes(m: int, f: int, k: int) -> int:
 
 
 def sdq_gated_linear(x, gate, up, act: int, h, workspace, stream=None, g=None, u=None) -> None:
-    """h = act(x gate^T) * (x up^T), all of x's type; g and u [m, f] also keep the projections."""
+    """h = act(x gate^T) * (x up^T), all of x's type; g and u [m, f] (of that type or fp32) also keep the
+    projections."""
     f, k = gate.shape
-    status = _call_gated_linear(x.data_ptr(), _DTYPES[x.dtype], x.shape[0], gate.data_ptr(), up.data_ptr(), f, k,
-                                int(act), h.data_ptr(), _ptr(g), _ptr(u), _ptr(workspace), _nbytes(workspace),
-                                _stream(stream))
+    t = _DTYPES[x.dtype]
+    status = _call_gated_linear(x.data_ptr(), t, x.shape[0], gate.data_ptr(), up.data_ptr(), f, k, int(act),
+                                h.data_ptr(), _ptr(g), _ptr(u), t if g is None else _DTYPES[g.dtype], _ptr(workspace),
+                                _nbytes(workspace), _stream(stream))
     if status != SDQ_OK:
         _check(status)
 
@@ -446,8 +448,8 @@ def sdq_gated_linear_backward(dh, x, gate, up, act: int, g, u, dx, dgate, dup, w
                               accumulate: bool = False) -> None:
     """Gradients of sdq_gated_linear for dh; dx may be None, and dgate with dup."""
     _check(_lib.sdq_gated_linear_backward(_ptr(dh), _ptr(x), _dtype_code(dh), dh.shape[0], _ptr(gate), _ptr(up),
-                                          gate.shape[0], gate.shape[1], int(act), _ptr(g), _ptr(u), _ptr(dx),
-                                          _ptr(dgate), _ptr(dup), int(bool(accumulate)), _ptr(workspace),
+                                          gate.shape[0], gate.shape[1], int(act), _ptr(g), _ptr(u), _dtype_code(g),
+                                          _ptr(dx), _ptr(dgate), _ptr(dup), int(bool(accumulate)), _ptr(workspace),
                                           _nbytes(workspace), _stream(stream)))
 
 
@@ -676,7 +678,7 @@ def int8_linear(x, w: Int8Rows, workspace=None, out=None, stream=None, accumulat
         if accumulate:
             raise ValueError("accumulate=True needs out")
         out = _empty((m, n), dtype or (torch.float16 if codes else x.dtype), w.q.device, stream)
-    _matrix("out", out, (m, n), _FLOATS if dtype is None else (dtype,), dev)
+    _matrix("out", out, (m, n), _FLOATS if dtype is None or dtype not in _FLOATS else (dtype,), dev)
     _with_workspace(lambda ws: sdq_int8_linear(x.q if codes else x, w.q, w.scales, out, ws, stream, accumulate,
                                                x.scales if codes else None),
                     workspace, lambda: sdq_int8_linear_workspace_bytes(m, n, k), w.q.device, stream)
@@ -696,7 +698,7 @@ def int8_gated_linear(x, gate: Int8Rows, up: Int8Rows, act: int = SDQ_ACT_SILU, 
     codes = isinstance(x, Int8Rows)
     if out is None:
         out = _empty((m, f), dtype or (torch.float16 if codes else x.dtype), gate.q.device, stream)
-    _matrix("out", out, (m, f), _FLOATS if dtype is None else (dtype,), dev)
+    _matrix("out", out, (m, f), _FLOATS if dtype is None or dtype not in _FLOATS else (dtype,), dev)
     _with_workspace(lambda ws: sdq_int8_gated_linear(x.q if codes else x, gate.q, gate.scales, up.q, up.scales, act,
                                                      out, ws, stream, x.scales if codes else None),
                     workspace, lambda: sdq_int8_gated_linear_workspace_bytes(m, f, k), gate.q.device, stream)
@@ -706,7 +708,7 @@ def int8_gated_linear(x, gate: Int8Rows, up: Int8Rows, act: int = SDQ_ACT_SILU, 
 def gated_linear(x, gate, up, act: int = SDQ_ACT_SILU, workspace=None, out=None, stream=None, g=None, u=None):
     """h = act(x gate^T) * (x up^T) for device matrices x [m, k], gate and up [f, k] of one type
     (fp16 or bf16).  g and u [m, f], given together, receive the projections, which
-    gated_linear_backward takes.  No autograd graph is recorded."""
+    gated_linear_backward takes: rounded to that type, or in fp32.  No autograd graph is recorded."""
     m, k = x.shape if x.dim() == 2 else (0, 0)
     f = gate.shape[0] if gate.dim() == 2 else 0
     t = (x.dtype,)
@@ -714,9 +716,13 @@ def gated_linear(x, gate, up, act: int = SDQ_ACT_SILU, workspace=None, out=None,
     _matrix("x", x, (m, k), _HALF, dev)
     _matrix("gate", gate, (f, k), t, dev)
     _matrix("up", up, (f, k), t, dev)
-    for name, v in (("out", out), ("g", g), ("u", u)):
-        if v is not None:
-            _matrix(name, v, (m, f), t, dev)
+    if out is not None:
+        _matrix("out", out, (m, f), t, dev)
+    if g is not None or u is not None:
+        if g is None or u is None:
+            raise ValueError("g and u are given together or not at all")
+        _matrix("g", g, (m, f), t + _FLOAT32, dev)
+        _matrix("u", u, (m, f), (g.dtype,), dev)
     h = out if out is not None else _empty((m, f), x.dtype, x.device, stream)
     _with_workspace(lambda ws: sdq_gated_linear(x, gate, up, act, h, ws, stream, g, u), workspace,
                     lambda: sdq_gated_linear_workspace_bytes(m, f, k), x.device, stream)
@@ -738,8 +744,9 @@ def gated_linear_backward(dh, x, gate, up, g, u, act: int = SDQ_ACT_SILU, worksp
     _matrix("x", x, (m, k), _HALF, dev)
     _matrix("gate", gate, (f, k), t, dev)
     _matrix("up", up, (f, k), t, dev)
-    for name, v in (("dh", dh), ("g", g), ("u", u)):
-        _matrix(name, v, (m, f), t, dev)
+    _matrix("dh", dh, (m, f), t, dev)
+    _matrix("g", g, (m, f), t + _FLOAT32, dev)
+    _matrix("u", u, (m, f), (g.dtype,), dev)
     if accumulate and need_weights and (dgate is None or dup is None):
         raise ValueError("accumulate=True needs dgate and dup")
     empty = lambda shape: _empty(shape, x.dtype, x.device, stream)

@@ -48,8 +48,9 @@ struct Product {
   int out_type = SDQ_F16;
   bool accumulate = false;
   int act = SDQ_ACT_SILU;
-  void* g_out = nullptr;   // gated: the projections themselves (16-bit, type elem), or NULL
+  void* g_out = nullptr;   // gated, 16-bit operands: the projections themselves, or NULL
   void* u_out = nullptr;
+  bool keep_f32 = false;   // in fp32 instead of elem
   // product_ws_bytes of workspace
   void* ws = nullptr;
   // The kernel, by plan_product from the sizes, the operands' rows and flags.
@@ -84,9 +85,9 @@ void launch_wide(const Product& p, hipStream_t stream);
 sdq_status launch_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t k, int8_t* q, int64_t ld,
                                 float* scales, hipStream_t stream);
 
-// dg = dh u act'(g) and du = dh act(g), [m x f], rounded to the type t of every operand; dg and du in
-// rows of ld (a multiple of 8), zeros past f.
-sdq_status launch_gate_gradient(const void* dh, const void* g, const void* u, sdq_dtype t, int64_t m, int64_t f,
-                                int64_t ld, int act, void* dg, void* du, hipStream_t stream);
+// dg = dh u act'(g) and du = dh act(g), [m x f], rounded to dh's type t; g and u of type kt (t or F32);
+// dg and du in rows of ld (a multiple of 8), zeros past f.
+sdq_status launch_gate_gradient(const void* dh, const void* g, const void* u, sdq_dtype t, sdq_dtype kt, int64_t m,
+                                int64_t f, int64_t ld, int act, void* dg, void* du, hipStream_t stream);
 
 }  // namespace sdq

@@ -238,8 +238,8 @@ size_t sdq_gated_linear_workspace_bytes(int64_t m, int64_t f, int64_t k) {
 }
 
 sdq_status sdq_gated_linear(const void* x, sdq_dtype t, int64_t m, const void* gate, const void* up, int64_t f,
-                            int64_t k, int32_t act, void* h, void* g, void* u, void* ws, size_t ws_bytes,
-                            void* stream) {
+                            int64_t k, int32_t act, void* h, void* g, void* u, sdq_dtype kt, void* ws,
+                            size_t ws_bytes, void* stream) {
   if (!float_type(t)) return set_error(SDQ_ERR_ARG, "bad dtype");
   if (!half_type(t)) return set_error(SDQ_ERR_UNSUPPORTED, "the dense block takes fp16 or bf16");
   if (!known_act(act)) return set_error(SDQ_ERR_ARG, "act %d is not an sdq_act", act);
@@ -247,6 +247,7 @@ sdq_status sdq_gated_linear(const void* x, sdq_dtype t, int64_t m, const void* g
   if (st != SDQ_OK || m == 0 || f == 0) return st;
   if (!x || !gate || !up || !h) return set_error(SDQ_ERR_ARG, "NULL pointer argument");
   if (!g != !u) return set_error(SDQ_ERR_ARG, "g and u are given together or not at all");
+  if (g && kt != t && kt != SDQ_F32) return set_error(SDQ_ERR_ARG, "g and u are of the block's type or fp32");
   if (!aligned16(x) || !aligned16(gate) || !aligned16(up) || !aligned16(h) || !aligned16(g) || !aligned16(u))
     return set_error(SDQ_ERR_ARG, "x, gate, up, h, g and u must be 16-byte aligned");
   Product p = gated_product(t, m, f, k);
@@ -259,6 +260,7 @@ sdq_status sdq_gated_linear(const void* x, sdq_dtype t, int64_t m, const void* g
   p.out[0] = h;
   p.g_out = g;
   p.u_out = u;
+  p.keep_f32 = kt == SDQ_F32;
   p.act = act;
   return launch_product(p, static_cast<hipStream_t>(stream));
 }
@@ -270,13 +272,14 @@ size_t sdq_gated_linear_backward_workspace_bytes(int64_t m, int64_t f, int64_t k
 
 sdq_status sdq_gated_linear_backward(const void* dh, const void* x, sdq_dtype t, int64_t m, const void* gate,
                                      const void* up, int64_t f, int64_t k, int32_t act, const void* g, const void* u,
-                                     void* dx, void* dgate, void* dup, int32_t accumulate, void* ws, size_t ws_bytes,
+                                     sdq_dtype kt, void* dx, void* dgate, void* dup, int32_t accumulate, void* ws, size_t ws_bytes,
                                      void* stream) {
   if (!float_type(t)) return set_error(SDQ_ERR_ARG, "bad dtype");
   if (!half_type(t)) return set_error(SDQ_ERR_UNSUPPORTED, "the dense block takes fp16 or bf16");
   if (!known_act(act)) return set_error(SDQ_ERR_ARG, "act %d is not an sdq_act", act);
   sdq_status st = check_sizes(m, f, k, false);
   if (st != SDQ_OK) return st;
+  if (kt != t && kt != SDQ_F32) return set_error(SDQ_ERR_ARG, "g and u are of the block's type or fp32");
   if (!dgate != !dup) return set_error(SDQ_ERR_ARG, "dgate and dup are given together or not at all");
   if (m > 0 && f > 0 && (!dh || !g || !u)) return set_error(SDQ_ERR_ARG, "NULL pointer argument");
   if ((dx && m > 0 && f > 0 && (!gate || !up)) || (dgate && m > 0 && f > 0 && !x))
@@ -290,7 +293,7 @@ sdq_status sdq_gated_linear_backward(const void* dh, const void* x, sdq_dtype t,
   const hipStream_t hs = static_cast<hipStream_t>(stream);
   if (!dx && !dgate) return SDQ_OK;
   if (m > 0 && f > 0) {
-    st = launch_gate_gradient(dh, g, u, t, m, f, s.ld, act, s.dg, s.du, hs);
+    st = launch_gate_gradient(dh, g, u, t, kt, m, f, s.ld, act, s.dg, s.du, hs);
     if (st != SDQ_OK) return st;
   }
   // Without rows or features the sums are empty: the products write zeros.

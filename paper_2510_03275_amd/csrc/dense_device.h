@@ -130,7 +130,10 @@ __device__ inline void finish4(const Product& p, int z, int64_t i, int64_t r, co
     for (int v = 0; v < 4; ++v) h[v] = act_value(g[v], p.act) * u[v];
     store4<TYPE>(p.out[0], i, r, p.cols, false, h);
     if constexpr (ELEM != kElemI8) {
-      if (p.g_out) {      // in the operands' own type, which is h's
+      if (p.g_out && p.keep_f32) {
+        store4<SDQ_F32>(p.g_out, i, r, p.cols, false, g);
+        store4<SDQ_F32>(p.u_out, i, r, p.cols, false, u);
+      } else if (p.g_out) {      // in the operands' own type, which is h's
         store4<TYPE>(p.g_out, i, r, p.cols, false, g);
         store4<TYPE>(p.u_out, i, r, p.cols, false, u);
       }

@@ -53,9 +53,9 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(PadJobs jobs) {
 // dg and du, eight elements of a row per thread; rows of dg and du hold ld elements, those past f zeros.
 // A row's last eight start earlier where eight more would pass its end: both threads find the same values.
 // Bound by memory: 4096 x 11008 bf16 (450 MB) in 81 us, 5.5 TB/s.
-template <class S>
-__global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict__ dh, const S* __restrict__ g,
-                                                            const S* __restrict__ u, int64_t m, int64_t f, int64_t ld,
+template <class S, class K>
+__global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict__ dh, const K* __restrict__ g,
+                                                            const K* __restrict__ u, int64_t m, int64_t f, int64_t ld,
                                                             int act, S* __restrict__ dg, S* __restrict__ du) {
   const int64_t o = blockIdx.x * int64_t{256} + threadIdx.x, per = ld / 8;
   if (o >= m * per) return;
@@ -65,17 +65,18 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict_
   const bool last = c + 8 >= f;
   c = last ? f - n : c;
   const int64_t i = row * f + c, at = row * ld + c;
-  S a[8], b[8], d[8], x[8], y[8];
+  S a[8], x[8], y[8];
+  K b[8], d[8];
   if (n == 8) {      // rows of f elements need not start aligned
-    __builtin_memcpy(a, dh + i, 16);
-    __builtin_memcpy(b, g + i, 16);
-    __builtin_memcpy(d, u + i, 16);
+    __builtin_memcpy(a, dh + i, sizeof(a));
+    __builtin_memcpy(b, g + i, sizeof(b));
+    __builtin_memcpy(d, u + i, sizeof(d));
   } else {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
       a[j] = j < n ? dh[i + j] : S(0);
-      b[j] = j < n ? g[i + j] : S(0);
-      d[j] = j < n ? u[i + j] : S(0);
+      b[j] = j < n ? g[i + j] : K(0);
+      d[j] = j < n ? u[i + j] : K(0);
     }
   }
 #pragma unroll
@@ -199,17 +200,22 @@ sdq_status launch_product(const Product& given, hipStream_t stream) {
   return e == hipSuccess ? SDQ_OK : hip_error(e, "product launch");
 }
 
-sdq_status launch_gate_gradient(const void* dh, const void* g, const void* u, sdq_dtype t, int64_t m, int64_t f,
-                                int64_t ld, int act, void* dg, void* du, hipStream_t stream) {
-  const dim3 grid(static_cast<unsigned>((m * (ld / 8) + 255) / 256));
-  if (t == SDQ_F16)
-    gate_gradient_kernel<<<grid, 256, 0, stream>>>(static_cast<const _Float16*>(dh), static_cast<const _Float16*>(g),
-                                                   static_cast<const _Float16*>(u), m, f, ld, act,
-                                                   static_cast<_Float16*>(dg), static_cast<_Float16*>(du));
-  else
-    gate_gradient_kernel<<<grid, 256, 0, stream>>>(static_cast<const __bf16*>(dh), static_cast<const __bf16*>(g),
-                                                   static_cast<const __bf16*>(u), m, f, ld, act,
-                                                   static_cast<__bf16*>(dg), static_cast<__bf16*>(du));
+namespace {
+template <class S, class K>
+void launch_gate(const void* dh, const void* g, const void* u, int64_t m, int64_t f, int64_t ld, int act, void* dg,
+                 void* du, hipStream_t stream) {
+  gate_gradient_kernel<<<dim3(static_cast<unsigned>((m * (ld / 8) + 255) / 256)), 256, 0, stream>>>(
+      static_cast<const S*>(dh), static_cast<const K*>(g), static_cast<const K*>(u), m, f, ld, act, static_cast<S*>(dg),
+      static_cast<S*>(du));
+}
+}  // namespace
+
+sdq_status launch_gate_gradient(const void* dh, const void* g, const void* u, sdq_dtype t, sdq_dtype kt, int64_t m,
+                                int64_t f, int64_t ld, int act, void* dg, void* du, hipStream_t stream) {
+  if (t == SDQ_F16 && kt == SDQ_F32) launch_gate<_Float16, float>(dh, g, u, m, f, ld, act, dg, du, stream);
+  else if (t == SDQ_F16) launch_gate<_Float16, _Float16>(dh, g, u, m, f, ld, act, dg, du, stream);
+  else if (kt == SDQ_F32) launch_gate<__bf16, float>(dh, g, u, m, f, ld, act, dg, du, stream);
+  else launch_gate<__bf16, __bf16>(dh, g, u, m, f, ld, act, dg, du, stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SDQ_OK : hip_error(e, "gate gradient launch");
 }

@@ -90,7 +90,7 @@ typedef sdq_status (*int8_gated_fn)(const void*, sdq_dtype, const float*, int64_
                                     const int8_t*, const float*, int64_t, int64_t, int32_t, void*, sdq_dtype, void*,
                                     size_t, void*);
 typedef sdq_status (*gated_fn)(const void*, sdq_dtype, int64_t, const void*, const void*, int64_t, int64_t, int32_t, void*,
-                               void*, void*, void*, size_t, void*);
+                               void*, void*, sdq_dtype, void*, size_t, void*);
 
 static int8_fn p_int8;
 static int8_gated_fn p_int8_gated;
@@ -133,14 +133,14 @@ static PyObject* py_int8_gated_linear(PyObject* self, PyObject* const* args, Py_
 }
 
 static PyObject* py_gated_linear(PyObject* self, PyObject* const* args, Py_ssize_t n) {
-  unsigned long long a[14];
+  unsigned long long a[15];
   sdq_status st;
   (void)self;
-  if (take(args, n, 14, a)) return NULL;
+  if (take(args, n, 15, a)) return NULL;
   Py_BEGIN_ALLOW_THREADS
   st = p_gated(PTR(const void*, 0), (sdq_dtype)a[1], (int64_t)a[2], PTR(const void*, 3), PTR(const void*, 4),
-               (int64_t)a[5], (int64_t)a[6], (int32_t)a[7], PTR(void*, 8), PTR(void*, 9), PTR(void*, 10), PTR(void*, 11),
-               (size_t)a[12], PTR(void*, 13));
+               (int64_t)a[5], (int64_t)a[6], (int32_t)a[7], PTR(void*, 8), PTR(void*, 9), PTR(void*, 10), (sdq_dtype)a[11],
+               PTR(void*, 12), (size_t)a[13], PTR(void*, 14));
   Py_END_ALLOW_THREADS
   return PyLong_FromLong((long)st);
 }

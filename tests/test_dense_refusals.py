@@ -24,9 +24,10 @@ QUANT = dict(x=A, xt=F16, m=2, k=8, q=A, s=A, stream=None)
 LINEAR = dict(x=A, xt=F16, xs=None, m=2, w=A, ws=A, n=4, k=8, y=A, yt=F16, acc=0, space=A, bytes=1 << 30, stream=None)
 GATED8 = dict(x=A, xt=F16, xs=None, m=2, g=A, gs=A, u=A, us=A, f=4, k=8, act=0, h=A, ht=F16, space=A, bytes=1 << 30,
               stream=None)
-GATED = dict(x=A, t=F16, m=2, gate=A, up=A, f=4, k=8, act=0, h=A, g=None, u=None, space=A, bytes=1 << 30, stream=None)
-BACK = dict(dh=A, x=A, t=F16, m=2, gate=A, up=A, f=4, k=8, act=0, g=A, u=A, dx=A, dgate=A, dup=A, acc=0, space=A,
-            bytes=1 << 30, stream=None)
+GATED = dict(x=A, t=F16, m=2, gate=A, up=A, f=4, k=8, act=0, h=A, g=None, u=None, kt=F16, space=A, bytes=1 << 30,
+             stream=None)
+BACK = dict(dh=A, x=A, t=F16, m=2, gate=A, up=A, f=4, k=8, act=0, g=A, u=A, kt=F16, dx=A, dgate=A, dup=A, acc=0,
+            space=A, bytes=1 << 30, stream=None)
 
 
 @pytest.mark.parametrize("name,args,change,status", [
@@ -50,7 +51,8 @@ BACK = dict(dh=A, x=A, t=F16, m=2, gate=A, up=A, f=4, k=8, act=0, g=A, u=A, dx=A
     ("sdq_gated_linear", GATED, dict(t=F32), UNSUPPORTED), ("sdq_gated_linear", GATED, dict(t=7), ARG),
     ("sdq_gated_linear", GATED, dict(act=-1), ARG), ("sdq_gated_linear", GATED, dict(g=A), ARG),
     ("sdq_gated_linear", GATED, dict(up=None), ARG), ("sdq_gated_linear", GATED, dict(x=A + 2), ARG),
-    ("sdq_gated_linear", GATED, dict(g=A, u=A + 2), ARG), ("sdq_gated_linear", GATED, dict(k=-3), ARG),
+    ("sdq_gated_linear", GATED, dict(g=A, u=A, kt=BF16), ARG), ("sdq_gated_linear_backward", BACK, dict(kt=BF16), ARG),
+    ("sdq_gated_linear_backward", BACK, dict(kt=3), ARG), ("sdq_gated_linear", GATED, dict(g=A, u=A + 2), ARG), ("sdq_gated_linear", GATED, dict(k=-3), ARG),
     ("sdq_gated_linear_backward", BACK, dict(t=F32), UNSUPPORTED), ("sdq_gated_linear_backward", BACK, dict(act=9), ARG),
     ("sdq_gated_linear_backward", BACK, dict(dgate=None), ARG), ("sdq_gated_linear_backward", BACK, dict(g=None), ARG),
     ("sdq_gated_linear_backward", BACK, dict(dh=None), ARG), ("sdq_gated_linear_backward", BACK, dict(gate=None), ARG),

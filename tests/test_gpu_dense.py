@@ -158,6 +158,11 @@ def test_gated_linear(m, f, k, dtype, act):
     assert torch.equal(h, h2) and ok() and ok2() and ok3() and ok4()
     D.assert_close(kg, g, eg + D.half(dtype) * (g.abs() + eg) + D.floor(dtype), "g")
     D.assert_close(ku, u, eu + D.half(dtype) * (u.abs() + eu) + D.floor(dtype), "u")
+    (kg, ok3), (ku, ok4) = (_guarded((m, f), F32) for _ in range(2))
+    P.gated_linear(x.cuda(), wg.cuda(), wu.cuda(), act, out=h2, g=kg, u=ku)
+    assert torch.equal(h, h2) and ok2() and ok3() and ok4()
+    D.assert_close(kg, g, eg, "g in fp32")
+    D.assert_close(ku, u, eu, "u in fp32")
 
 
 @pytest.mark.parametrize("m,f,k", SIZES + LARGE)
@@ -182,6 +187,10 @@ def test_gated_backward(m, f, k, dtype, act):
     a, b, c = P.gated_linear_backward(*dev, act, need_dx=False)
     assert a is None and torch.equal(b, dg) and torch.equal(c, du)
     assert all(o[1]() for o in outs)
+    g32, u32 = ((D.rand(m + i, m, f) * 2).float() for i in range(1, 3))
+    got = P.gated_linear_backward(*dev[:4], g32.cuda(), u32.cuda(), act)
+    for v, (r, b), what in zip(got, D.backward_ref(dh, x, wg, wu, g32, u32, act, dtype), ("dx", "dgate", "dup")):
+        D.assert_close(v, r, b, what + " from g and u in fp32")
     dg.copy_(base[0])
     du.copy_(base[1])
     P.gated_linear_backward(*dev, act, dgate=dg, dup=du, accumulate=True)
@@ -249,6 +258,72 @@ def test_empty():
     dx = torch.full((2, 8), 5.0, dtype=F16, device="cuda")
     P.gated_linear_backward(z(2, 0), z(2, 8), z(0, 8), z(0, 8), z(2, 0), z(2, 0), dx=dx)
     assert not bool(dx.any())
+
+
+@pytest.mark.parametrize("k", [7, 9, 40])
+def test_empty_sums(k):
+    """No rows: zero gradients of the weights; no features: a zero dx (rows aligned and not)."""
+    require_gpu()
+    import paper_2510_03275_amd as P
+    z = lambda *s: torch.zeros(*s, dtype=BF16, device="cuda")
+    out = [torch.full((5, k), 5.0, dtype=BF16, device="cuda") for _ in range(2)]
+    P.gated_linear_backward(z(0, 5), z(0, k), z(5, k), z(5, k), z(0, 5), z(0, 5), dgate=out[0], dup=out[1])
+    assert not any(bool(o.any()) for o in out)
+    dx = torch.full((70, k), 5.0, dtype=BF16, device="cuda")
+    P.gated_linear_backward(z(70, 0), z(70, k), z(0, k), z(0, k), z(70, 0), z(70, 0), dx=dx)
+    assert not bool(dx.any())
+
+
+@pytest.mark.parametrize("m,f,k", [(1, 48, 64), (16, 96, 1001), (24, 520, 640), (60, 300, 999), (70, 300, 999),
+                                   (200, 640, 2048), (300, 260, 1003), (1000, 520, 4096)])
+def test_workspaces_of_the_stated_size(m, f, k):
+    """Every call on a workspace of exactly the bytes it asks for: nothing behind it is written, and what
+    it held before does not matter."""
+    require_gpu()
+    import paper_2510_03275_amd as P
+    x, dh = D.rand(1, m, k).to(F16).cuda(), D.rand(2, m, f).to(F16).cuda()
+    wg, wu = (D.rand(i, f, k, scale=k ** -0.5).to(F16).cuda() for i in (3, 4))
+    g, u = (D.rand(i, m, f).to(F16).cuda() for i in (5, 6))
+    g8, u8 = P.int8_quantize(wg), P.int8_quantize(wu)
+    x8 = P.int8_quantize(x)
+    calls = [(P.sdq_int8_linear_workspace_bytes(m, f, k), lambda ws: [P.int8_linear(x, g8, workspace=ws)]),
+             (P.sdq_int8_linear_workspace_bytes(m, f, k), lambda ws: [P.int8_linear(x8, g8, workspace=ws)]),
+             (P.sdq_int8_gated_linear_workspace_bytes(m, f, k),
+              lambda ws: [P.int8_gated_linear(x, g8, u8, workspace=ws)]),
+             (P.sdq_gated_linear_workspace_bytes(m, f, k), lambda ws: [P.gated_linear(x, wg, wu, workspace=ws)]),
+             (P.sdq_gated_linear_backward_workspace_bytes(m, f, k),
+              lambda ws: P.gated_linear_backward(dh, x, wg, wu, g, u, workspace=ws))]
+    for need, call in calls:
+        want = call(None)
+        for fill in (0, 255):
+            buf = torch.full((need + 4096,), fill, dtype=torch.uint8, device="cuda")
+            got = call(buf[:need])
+            assert all(torch.equal(a, b) for a, b in zip(got, want)) and bool((buf[need:] == fill).all())
+
+
+def test_refusals_on_the_device():
+    require_gpu()
+    import paper_2510_03275_amd as P
+    x = torch.zeros(8, 16, dtype=F16, device="cuda")
+    w8 = P.int8_quantize(torch.ones(4, 16, device="cuda"))
+    w = torch.zeros(4, 16, dtype=F16, device="cuda")
+    h, h32 = torch.zeros(8, 4, dtype=F16, device="cuda"), torch.zeros(8, 4, device="cuda")
+    for bad in (lambda: P.int8_quantize(x.t()), lambda: P.int8_quantize(x[0]), lambda: P.int8_quantize(x.double()),
+                lambda: P.int8_linear(x[:, :8], w8), lambda: P.int8_linear(x, w8, accumulate=True),
+                lambda: P.int8_linear(x, w8, out=h.t()), lambda: P.int8_linear(x, w8, dtype=torch.float64),
+                lambda: P.int8_linear(x, w8, out=h, dtype=F32), lambda: P.int8_linear(x, P.Int8Rows(w8.q, w8.scales[:3])),
+                lambda: P.int8_linear(x.cpu(), w8), lambda: P.int8_gated_linear(x, w8, P.int8_quantize(w[:3])),
+                lambda: P.gated_linear(x.float(), w.float(), w.float()), lambda: P.gated_linear(x, w, w.bfloat16()),
+                lambda: P.gated_linear(x, w, w, g=h), lambda: P.gated_linear(x, w, w, g=h, u=h32),
+                lambda: P.gated_linear_backward(h, x, w, w, h.bfloat16(), h.bfloat16()),
+                lambda: P.gated_linear_backward(h, x, w, w, h, h, accumulate=True),
+                lambda: P.gated_linear_backward(h, x, w, w, h, h, dx=x[:4])):
+        with pytest.raises(ValueError):
+            bad()
+    with pytest.raises(P.SdqError):          # starts 2 bytes off
+        P.int8_quantize(torch.zeros(65, dtype=F16, device="cuda")[1:].view(4, 16))
+    with pytest.raises(P.SdqError):
+        P.gated_linear(x, w, w, act=3)
 
 
 def _ffn_step(P, t, m, f, k, seed=0):
