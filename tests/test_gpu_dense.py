@@ -367,6 +367,18 @@ def test_graph_replays_match_eager(m, f, k):
         torch.cuda.synchronize()
 
 
+@pytest.mark.parametrize("m,f,k", [(2, 1000, 4096), (50, 1000, 8192), (130, 2000, 4096), (2100, 4200, 2048)])
+def test_every_run_gives_the_same_bits(m, f, k):
+    """Long depths on every kernel and tile height, twenty times with other work between."""
+    require_gpu()
+    import paper_2510_03275_amd as P
+    step = _ffn_step(P, BF16, m, f, k)
+    want = [v.clone() for v in step()]
+    for rep in range(20):
+        torch.empty(1 << 26, dtype=torch.uint8, device="cuda").fill_(rep)
+        assert all(torch.equal(a, b) for a, b in zip(step(), want)), rep
+
+
 @pytest.mark.parametrize("m", [1, 30, 300])
 def test_graphs_share_a_workspace(m):
     """Two graphs captured on one workspace, replayed in turn on one stream, with eager calls on it between."""
