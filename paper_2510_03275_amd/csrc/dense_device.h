@@ -55,16 +55,16 @@ constexpr float kGeluB = 0.07135481282053126f;       // 0.044715 of it
 __device__ inline float act_arg(float g, int act) {
   return act == SDQ_ACT_SILU ? g : g * (kGeluA + kGeluB * g * g);
 }
-// e^-a, clamped where it is 0 or inf anyway.  The exponent -a log2(e) is off by 2^-24 of itself, so its power
-// is off by |a| 2^-24 of itself: 2^-20 at |a| = 16, 5e-6 at 88, far below a 16-bit output's rounding.  PRECISE adds
-// the product's rest, for outputs in fp32.  With the library's function a turn of 256 x 128 gated tiles took 2 us
-// more of the 12 it spends outside its steps (2048 x 28672 outputs at K = 128: 107 us, now 93).
+// e^-a.  The exponent -a log2(e) is off by 2^-24 of itself, so its power is off by
+// |a| 2^-24 of itself: 2^-20 at |a| = 16, 5e-6 at 88, far below a 16-bit output's rounding.  PRECISE adds the
+// product's rest (a is clamped where e^-a is 0 or inf anyway), for outputs in fp32.  With the library's
+// function 2048 x 28672 gated outputs at K = 128 took 107 us instead of 93.
 template <bool PRECISE>
 __device__ inline float exp_minus(float a) {
   constexpr float kLog2e = 1.4426950408889634f, kRest = 1.9259629911266175e-8f;      // log2(e) = their sum
-  const float c = __builtin_amdgcn_fmed3f(a, -104.0f, 104.0f), t = -c * kLog2e;
+  if (!PRECISE) return __builtin_amdgcn_exp2f(-kLog2e * a);
+  const float c = __builtin_amdgcn_fmed3f(a, -104.0f, 104.0f), t = -c * kLog2e;      // t is finite
   const float e = __builtin_amdgcn_exp2f(t);
-  if (!PRECISE) return e;
   const float rest = __builtin_fmaf(-c, kLog2e, -t) - c * kRest;
   return e < 3e38f ? __builtin_fmaf(e, rest * 0.6931471805599453f, e) : e;
 }
@@ -108,6 +108,23 @@ __device__ inline void store4(void* out, int64_t i, int64_t r, int64_t cols, boo
 #pragma unroll
   for (int j = 0; j < 4; ++j)
     if (r + j < cols) at[j] = static_cast<S>(accumulate ? static_cast<float>(at[j]) + v[j] : v[j]);
+}
+
+// 16 bytes of outputs from r on: four in fp32, eight of 16 bits.
+template <int TYPE>
+__device__ inline void store16(void* out, int64_t i, int64_t r, int64_t cols, i32x4 v) {
+  if constexpr (TYPE == SDQ_F32) {
+    store4<TYPE>(out, i, r, cols, false, __builtin_bit_cast(f32x4, v));
+  } else {
+    uint16_t* at = static_cast<uint16_t*>(out) + i * cols + r;
+    if (r + 8 <= cols) {
+      __builtin_memcpy(at, &v, 16);
+      return;
+    }
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (r + j < cols) at[j] = static_cast<uint16_t>(static_cast<unsigned>(v[j / 2]) >> 16 * (j % 2));
+  }
 }
 
 // The scales of four rows of wide (of gate and of up), for 8-bit operands.

@@ -30,10 +30,8 @@
 //             elements); a group of 16 lanes reads 4 depths x 16 elements
 //             transposed (ds_read_b64_tr_b16), 32-byte granule p of depth c at
 //             p ^ (2 (c % 4) + c / 8 % 2).  So the gradients need no transposed copies in memory.
-//   outputs   The sums go through LDS, up to 128 rows at a time, so that the stores are
-//             whole rows and the code that scales, activates and converts exists once
-//             (unrolled over a lane's 128 sums it was 130 KB of instructions, whose
-//             first fetch took 20 us).
+//   outputs   Scaled and activated in registers (a wave's columns of gate and of up are the same ones),
+//             then through LDS in their own type, so that the stores are whole rows.
 //   splits    Where the tiles are fewer than the compute units, the depth is cut and
 //             the sums of every part go to the workspace; join_kernel adds them in
 //             order.  Where they are a turn of the chip and a part of one, the last rows
@@ -168,8 +166,9 @@ struct Loader {
   }
 };
 
-// The lane's places in an operand's step for a wave's 16 N rows from row0 on.
-template <bool STRIDED, int N>
+// The lane's places in an operand's step for a wave's 16 N rows from row0 on (HALVES: for half of them
+// there and half 128 rows further on).
+template <bool STRIDED, bool HALVES, int N>
 struct Frags {
   int at[STRIDED ? N : 2];
   __device__ inline void init(int row0, int lane) {
@@ -191,7 +190,8 @@ struct Frags {
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4)(p + 1024));
       return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      return *reinterpret_cast<const i32x4*>(lds + at[s] + n * 16 * kStepBytes);
+      const int row = HALVES && n >= N / 2 ? 128 + 16 * (n - N / 2) : 16 * n;
+      return *reinterpret_cast<const i32x4*>(lds + at[s] + row * kStepBytes);
     }
   }
 };
@@ -204,6 +204,50 @@ template <> struct Stages<64> { static constexpr int kTall = 4, kWide = 4; };
 
 template <int TALL>
 constexpr int kLdsBytes = (Stages<TALL>::kTall * TALL + Stages<TALL>::kWide * 256) * kStepBytes;
+
+// Where a lane's outputs lie: its tile's origin and its row in it.
+struct Tile {
+  int64_t row0, col0;
+  int lr, lane, tid;
+};
+
+// Stores a tile's TALL x COLS outputs, value(i, j) in rows lr + 16 i and columns lc[j] .. + 3 of it, by
+// place(row, column, 16 bytes).  They pass LDS in type VIA, half the tile at a time where it holds no more, so that the
+// stores are whole rows: lines of COLS values whose 16-byte chunk q of line r lies at q ^ (r % 16).
+template <int VIA, int TALL, int COLS, int LDS, class Value, class Place>
+__device__ __forceinline__ void store_tile(const Product& p, const Tile& t, char* lds, const int (&lc)[4], Value value,
+                                           Place place) {
+  using Four = typename Out<VIA>::Four;
+  constexpr int kSize = VIA == SDQ_F32 ? 4 : 2, kLine = COLS * kSize, kPer = 16 / kSize, kChunks = kLine / 16;
+  constexpr int kPasses = TALL * kLine > LDS ? 2 : 1, kFrags = TALL / 32 / kPasses, kRows = TALL / 2 / kPasses;
+  constexpr int kLines = 512 / kChunks, kTurns = 2 * kRows / kLines;
+  static_assert(2 * kRows * kLine <= LDS && kChunks >= 16 && kTurns > 0 && kTurns * kLines == 2 * kRows, "whole turns");
+  const int q = t.tid % kChunks, first = t.tid / kChunks, wt = t.lr / (TALL / 2);
+  const int64_t c = t.col0 + kPer * q;
+#pragma unroll
+  for (int pass = 0; pass < kPasses; ++pass) {
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kFrags; ++i) {
+      __builtin_amdgcn_sched_barrier(0);      // row by row: there are no registers for all at once
+#pragma unroll
+      for (int j = 0; j < COLS / 64; ++j) {
+        const int r = kRows * wt + 16 * i + t.lane % 16, at = lc[j] * kSize;
+        *reinterpret_cast<Four*>(lds + r * kLine + ((at / 16) ^ (t.lane % 16)) * 16 + at % 16) =
+            __builtin_convertvector(value(kFrags * pass + i, j), Four);
+      }
+    }
+    __syncthreads();
+    if (c >= p.cols) continue;
+#pragma unroll 4
+    for (int n = 0; n < kTurns; ++n) {
+      const int r = first + n * kLines;
+      const int64_t row = t.row0 + TALL / 2 * (r / kRows) + kRows * pass + r % kRows;
+      const char* src = lds + r * kLine + (q ^ (r % 16)) * 16;
+      if (row < p.rows) place(row, c, *reinterpret_cast<const i32x4*>(src));
+    }
+  }
+}
 
 // One tile of the rows from first_row on, `index` of the `total` workgroups that share them.
 template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED, int TALL>
@@ -245,10 +289,10 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
   Loader<kB, WIDE_STRIDED, GATED, 256> lb;
   la.init(p.tall[p.batch > 1 ? z : 0], p.tall[1], row0, p.rows, p.ld_tall, p.depth, t0, seg_steps, wave, lane);
   lb.init(p.wide[0], p.wide[1], col0, p.cols, p.ld_wide, p.depth, t0, seg_steps, wave, lane);
-  Frags<TALL_STRIDED, kFrags> fa;
-  Frags<WIDE_STRIDED, 4> fb;
+  Frags<TALL_STRIDED, false, kFrags> fa;
+  Frags<WIDE_STRIDED, GATED, 4> fb;
   fa.init(TALL / 2 * wt, lane);
-  fb.init(64 * ww, lane);
+  fb.init((GATED ? 32 : 64) * ww, lane);
 
   // LDS offsets of the stages read and filled next.
   int get_a = 0, get_b = kWide, put_a = 0, put_b = kWide;
@@ -337,54 +381,81 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
   int t = t0;
   for (; t + kWideStages < whole; ++t) step(t, std::false_type());
   for (; t < t1; ++t) step(t, std::true_type());
-  __builtin_amdgcn_s_waitcnt(0);      // the copies past the end land before the sums take their place
-  __syncthreads();
+  __builtin_amdgcn_s_waitcnt(0);      // the copies past the end land before outputs take their place
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
 
-  // Sums of (up to) 64 rows of either half of tall: [rows][64 chunks of four columns], chunk q of
-  // row r at q ^ (r % 16).
-  constexpr int kRows = TALL / 2 < 64 ? TALL / 2 : 64, kPasses = TALL / 2 / kRows;
-  Acc* sums = reinterpret_cast<Acc*>(lds);
-  float* row_scales = reinterpret_cast<float*>(lds + 2 * kRows * 1024);      // of the tile's rows of tall
-  static_assert(2 * kRows * 1024 + TALL * 4 <= kEnd, "the sums and scales fit");
-  if (ELEM == kElemI8 && tid < TALL) row_scales[tid] = p.tall_scale[min(row0 + tid, p.rows - 1)];
-  const int64_t ld_part = (p.cols + 3) / 4 * 4;      // of gate and of up
-  constexpr int kOuts = GATED ? 32 : 64, kTurns = 2 * kRows * kOuts / 512;
-  // A thread's outputs lie in one chunk of columns.
-  const int q = tid % kOuts;
-  const int64_t c = col0 + 4 * q;
-  WideScales<ELEM, GATED> wide_scales;
-  if (splits == 1) wide_scales.load(p, c);
+  // The lane's sums: rows lr + 16 i of the tile, columns lc[j] .. + 3 (of gate, of up).
+  const int lr = TALL / 2 * wt + lane % 16;
+  int lc[4];
 #pragma unroll
-  for (int pass = 0; pass < kPasses; ++pass) {
-    if (pass) __syncthreads();
+  for (int j = 0; j < 4; ++j) lc[j] = (GATED ? 32 * ww + 16 * (j % 2) : 64 * ww + 16 * j) + 4 * (lane / 16);
+  const Tile tile_out = {row0, col0, lr, lane, tid};
+  if (splits > 1) {
+    const int64_t ld = (p.cols + 3) / 4;      // of gate and of up, in fours
 #pragma unroll
-    for (int i = 0; i < kRows / 16; ++i)
+    for (int half = 0; half < (GATED ? 2 : 1); ++half)
+      store_tile<SDQ_F32, TALL, kCols, kEnd>(
+          p, tile_out, lds, lc, [&](int i, int j) { return __builtin_bit_cast(f32x4, acc[i][j + 2 * half]); },
+          [&](int64_t row, int64_t c, i32x4 v) {
+            static_cast<i32x4*>(p.ws)[((part * p.rows + row) * (GATED ? 2 : 1) + half) * ld + c / 4] = v;
+          });
+    return;
+  }
+  float row_scale[kFrags];
+  f32x4 col_scale[4];
+  if constexpr (ELEM == kElemI8) {
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int r = kRows * wt + 16 * i + lane % 16, at = 16 * ww + 4 * j + lane / 16;
-        sums[r * 64 + (at ^ (r % 16))] = acc[kRows / 16 * pass + i][j];
+    for (int i = 0; i < kFrags; ++i) row_scale[i] = p.tall_scale[min(row0 + lr + 16 * i, p.rows - 1)];
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int v = 0; v < 4; ++v) col_scale[j][v] = p.wide_scale[GATED ? j / 2 : 0][min(col0 + lc[j] + v, p.cols - 1)];
+  }
+  auto sum = [&](int i, int j) { return as_floats<ELEM>(acc[i][j], row_scale[i], col_scale[j]); };
+  if constexpr (GATED) {
+    with_out_type<ELEM>(p, [&](auto type) {
+      constexpr int kType = decltype(type)::value;
+      auto put = [&](auto as, void* out, auto value) {
+        constexpr int kAs = decltype(as)::value;
+        store_tile<kAs, TALL, kCols, kEnd>(p, tile_out, lds, lc, value,
+                                           [&](int64_t row, int64_t c, i32x4 v) { store16<kAs>(out, row, c, p.cols, v); });
+      };
+      auto activated = [&](auto act) {
+        put(type, p.out[0], [&](int i, int j) {
+          f32x4 g = sum(i, j);
+          const f32x4 u = sum(i, j + 2);
+#pragma unroll
+          for (int v = 0; v < 4; ++v) g[v] = act_value<kType == SDQ_F32>(g[v], decltype(act)::value) * u[v];
+          return g;
+        });
+      };
+      if (p.act == SDQ_ACT_SILU) activated(std::integral_constant<int, SDQ_ACT_SILU>());
+      else activated(std::integral_constant<int, SDQ_ACT_GELU_TANH>());
+      if constexpr (ELEM != kElemI8) {
+        auto put_both = [&](auto as) {
+          put(as, p.g_out, sum);
+          put(as, p.u_out, [&](int i, int j) { return sum(i, j + 2); });
+        };
+        if (p.g_out && p.keep_f32) put_both(std::integral_constant<int, SDQ_F32>());
+        else if (p.g_out) put_both(type);      // in the operands' own type, which is h's
       }
-    __syncthreads();
-    if (c >= p.cols) continue;
-    auto outputs = [&](auto type) {
-#pragma unroll 4
-      for (int n = 0; n < kTurns; ++n) {
-        const int r = tid / kOuts + n * (512 / kOuts), tile_row = TALL / 2 * (r / kRows) + kRows * pass + r % kRows;
-        const int64_t row = row0 + tile_row;
-        const Acc a = sums[r * 64 + (q ^ (r % 16))], b = GATED ? sums[r * 64 + ((q + 32) ^ (r % 16))] : Acc{};
-        if (row >= p.rows) continue;
-        if constexpr (decltype(type)::value < 0) {
-          Acc* dst = static_cast<Acc*>(p.ws) + (part * p.rows + row) * ((GATED ? 2 : 1) * ld_part / 4) + c / 4;
-          dst[0] = a;
-          if (GATED) dst[ld_part / 4] = b;
-        } else {
-          finish4<ELEM, GATED, decltype(type)::value>(p, z, row, c, a, b, ELEM == kElemI8 ? row_scales[tile_row] : 1.0f,
-                                                      wide_scales);
-        }
+    });
+  } else {
+    with_out_type<ELEM>(p, [&](auto type) {
+      constexpr int kType = decltype(type)::value;
+      // What is added to is rounded once: its summands pass LDS in fp32.
+      if constexpr (ELEM == kElemI8 || TALL_STRIDED) {
+        if (p.accumulate)
+          return store_tile<SDQ_F32, TALL, kCols, kEnd>(
+              p, tile_out, lds, lc, sum, [&](int64_t row, int64_t c, i32x4 v) {
+                store4<kType>(p.out[z], row, c, p.cols, true, __builtin_bit_cast(f32x4, v));
+              });
       }
-    };
-    if (splits > 1) outputs(std::integral_constant<int, -1>());
-    else with_out_type<ELEM>(p, outputs);
+      store_tile<kType, TALL, kCols, kEnd>(p, tile_out, lds, lc, sum, [&](int64_t row, int64_t c, i32x4 v) {
+        store16<kType>(p.out[z], row, c, p.cols, v);
+      });
+    });
   }
 }
 
