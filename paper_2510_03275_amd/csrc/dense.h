@@ -11,7 +11,7 @@ enum ElemType { kElemF16 = SDQ_F16, kElemBf16 = SDQ_BF16, kElemI8 = 3 };
 
 // How a product is cut on tiles (dense_wide.hip): rows of tall to a tile and the parts of the depth.
 struct WidePlan {
-  int tall = 256, splits = 0;
+  int tall = 256, wide = 256, splits = 0;      // rows of a tile, parts of the depth
   int64_t mixed = 0;                  // tiles of 256 rows for so many of them, of 128 for the rest
   double us = 0;                      // about what it takes
 };

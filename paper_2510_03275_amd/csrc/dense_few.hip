@@ -246,11 +246,13 @@ bool few_quantizes(const Product& p) {
          p.rows * p.depth <= (p.rows == 1 ? kOwnCodes : kOwnCodes / 4);
 }
 
-// Fitted as wide_plan's times are, up to 15 % off at 16 rows: 4 us and the weights at 4.9 TB/s, longer by
+// Fitted as wide_plan's times are (what is picked of both takes 1.6 % longer than the faster one on average):
+// 3 us and the longer of two, the weights at 5.4 TB/s or a wave's way through the depth, both longer by
 // the rows' own reads, which from 17 rows on are more than the weights'.
 double few_us(const Product& p) {
-  const double bytes = static_cast<double>(p.cols) * p.depth * (p.gated ? 2 : 1) * (p.elem == kElemI8 ? 1 : 2);
-  return 4.0 + bytes / 4.9e6 * (1 + 0.015 * p.rows) * (p.rows > 16 ? 1.8 : 1.0);
+  const double row = static_cast<double>(p.depth) * (p.elem == kElemI8 ? 1 : 2), weights = row * p.cols * (p.gated ? 2 : 1);
+  const double us = std::max(weights / 5.4e6, row * (p.gated ? 1.7e-3 : 0.9e-3));
+  return 3.0 + us * (1 + 0.018 * p.rows) * (p.rows > 16 ? 1.5 : 1.0);
 }
 
 void launch_few(const Product& p, hipStream_t stream) {

@@ -1,5 +1,5 @@
-// The products of the dense operators on tiles of 256 rows of wide by 256, 128
-// or 64 rows of tall (dense.h), for operands whose rows start 16-byte aligned.
+// The products of the dense operators on tiles of 256 or 128 rows of wide by 256,
+// 128 or 64 rows of tall (dense.h), for operands whose rows start 16-byte aligned.
 //
 // What bounds it, at 256 x 256: a step of 128 bytes of depth keeps the matrix
 // cores of a SIMD for 2048 clocks; beside it go 192 KB of LDS reads (768 clocks), 64 KB
@@ -13,7 +13,10 @@
 //   tile      Eight waves, two to a SIMD; wave (wt, ww) forms half the rows of tall by
 //             64 of wide with 16 x 16 matrix instructions (128 x 64 in 128 registers).  (Four waves of
 //             128 x 128 on 32 x 32 instructions: 11 % slower, and twice the accumulator traffic.)  Of a
-//             gated product the tile's rows of wide are 128 of gate and the same 128 of up.
+//             gated product half the tile's rows of wide are gate's and half the same ones of up.
+//             With few rows of tall the weights' stream bounds it, which tiles of 128 rows of wide spread over
+//             twice the compute units: 64 rows against gate and up of 11008 x 4096 in 8 bits 24.7 us,
+//             with 256 32.4 or, in two splits, 26.9; 200 rows against 11008 x 4096 20.6 and 28.0.
 //   steps     The operands of half a step (64 bytes of depth) are read from LDS while the other
 //             half is multiplied, in the order in which the products ask for them; one barrier a step.
 //             (Reading and multiplying by turns in two halves of the workgroup: 6 % slower.)
@@ -91,8 +94,8 @@ __device__ inline void copy_16(char* lds, const char* src, int end, unsigned off
 // are 32 bits wide: no branch splits the loop.
 template <int BYTES, bool STRIDED, bool HALVES, int ROWS>
 struct Loader {
-  static_assert(ROWS == 256 || (!HALVES && !(STRIDED && ROWS == 64)), "halves of 128 rows");
-  static constexpr int kCopies = ROWS / 64;
+  static_assert(!(STRIDED && (HALVES || ROWS == 64)), "strided rows come by 128");
+  static constexpr int kCopies = ROWS / 64, kHalf = HALVES ? ROWS / 2 : ROWS;
   static constexpr int kStep = kStepBytes / BYTES;
   const char* src[HALVES ? 2 : 1];
   int num[HALVES ? 2 : 1];   // depth-contiguous: bytes from src to the last row's end
@@ -129,13 +132,13 @@ struct Loader {
       depth = static_cast<int>(depth_ * BYTES);
       src[0] = static_cast<const char*>(t < steps ? first : other) + at;
       second = static_cast<const char*>(other) + at;
-      num[0] = min(valid, HALVES ? 128 : ROWS) * static_cast<int>(ld_bytes);
+      num[0] = min(valid, kHalf) * static_cast<int>(ld_bytes);
       if (HALVES) {
         src[HALVES] = second;
         num[HALVES] = num[0];
       }
       chunk = 16 * ((lane % 8) ^ (lane / 8));
-      for (int j = 0; j < kCopies; ++j) off[j] = (8 * wave + lane / 8 + 64 * (HALVES ? j % 2 : j)) * ld_bytes + chunk;
+      for (int j = 0; j < kCopies; ++j) off[j] = (8 * wave + lane / 8 + 64 * j % kHalf) * ld_bytes + chunk;
       soff = past * kStepBytes;
       left = depth - soff;
       row_bytes = skip = 0;
@@ -153,7 +156,7 @@ struct Loader {
     const int have = MASK && !read ? 0 : left;
 #pragma unroll
     for (int j = 0; j < kCopies; ++j) {
-      const int h = HALVES ? j / 2 : 0;
+      const int h = 64 * j / kHalf;
       // Strided: columns behind the operand's last belong to the next depth: they are read, and their
       // outputs not stored.
       const int end = STRIDED ? max(min(have, kStep) * row_bytes - skip, 0) : num[h];
@@ -166,9 +169,9 @@ struct Loader {
   }
 };
 
-// The lane's places in an operand's step for a wave's 16 N rows from row0 on (HALVES: for half of them
-// there and half 128 rows further on).
-template <bool STRIDED, bool HALVES, int N>
+// The lane's places in an operand's step for a wave's 16 N rows from row0 on (HALF: for half of them
+// there and half HALF rows further on).
+template <bool STRIDED, int HALF, int N>
 struct Frags {
   int at[STRIDED ? N : 2];
   __device__ inline void init(int row0, int lane) {
@@ -190,20 +193,22 @@ struct Frags {
       const s16x4 hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((LdsS4)(p + 1024));
       return __builtin_bit_cast(i32x4, __builtin_shufflevector(lo, hi, 0, 1, 2, 3, 4, 5, 6, 7));
     } else {
-      const int row = HALVES && n >= N / 2 ? 128 + 16 * (n - N / 2) : 16 * n;
+      const int row = HALF && n >= N / 2 ? HALF + 16 * (n - N / 2) : 16 * n;
       return *reinterpret_cast<const i32x4*>(lds + at[s] + row * kStepBytes);
     }
   }
 };
 
 // Stages of LDS: as many as 160 KB hold.
-template <int TALL> struct Stages;
-template <> struct Stages<256> { static constexpr int kTall = 2, kWide = 3; };
-template <> struct Stages<128> { static constexpr int kTall = 3, kWide = 3; };
-template <> struct Stages<64> { static constexpr int kTall = 4, kWide = 4; };
+template <int TALL, int WIDE> struct Stages;
+template <> struct Stages<256, 256> { static constexpr int kTall = 2, kWide = 3; };
+template <> struct Stages<128, 256> { static constexpr int kTall = 3, kWide = 3; };
+template <> struct Stages<64, 256> { static constexpr int kTall = 4, kWide = 4; };
+template <> struct Stages<128, 128> { static constexpr int kTall = 5, kWide = 5; };
+template <> struct Stages<64, 128> { static constexpr int kTall = 6, kWide = 6; };
 
-template <int TALL>
-constexpr int kLdsBytes = (Stages<TALL>::kTall * TALL + Stages<TALL>::kWide * 256) * kStepBytes;
+template <int TALL, int WIDE>
+constexpr int kLdsBytes = (Stages<TALL, WIDE>::kTall * TALL + Stages<TALL, WIDE>::kWide * WIDE) * kStepBytes;
 
 // Where a lane's outputs lie: its tile's origin and its row in it.
 struct Tile {
@@ -213,15 +218,15 @@ struct Tile {
 
 // Stores a tile's TALL x COLS outputs, value(i, j) in rows lr + 16 i and columns lc[j] .. + 3 of it, by
 // place(row, column, 16 bytes).  They pass LDS in type VIA, half the tile at a time where it holds no more, so that the
-// stores are whole rows: lines of COLS values whose 16-byte chunk q of line r lies at q ^ (r % 16).
+// stores are whole rows: lines of COLS values whose 16-byte chunk q of line r lies at q ^ (r % 16) (% 8 of eight).
 template <int VIA, int TALL, int COLS, int LDS, class Value, class Place>
-__device__ __forceinline__ void store_tile(const Product& p, const Tile& t, char* lds, const int (&lc)[4], Value value,
+__device__ __forceinline__ void store_tile(const Product& p, const Tile& t, char* lds, const int* lc, Value value,
                                            Place place) {
   using Four = typename Out<VIA>::Four;
   constexpr int kSize = VIA == SDQ_F32 ? 4 : 2, kLine = COLS * kSize, kPer = 16 / kSize, kChunks = kLine / 16;
   constexpr int kPasses = TALL * kLine > LDS ? 2 : 1, kFrags = TALL / 32 / kPasses, kRows = TALL / 2 / kPasses;
-  constexpr int kLines = 512 / kChunks, kTurns = 2 * kRows / kLines;
-  static_assert(2 * kRows * kLine <= LDS && kChunks >= 16 && kTurns > 0 && kTurns * kLines == 2 * kRows, "whole turns");
+  constexpr int kLines = 512 / kChunks, kTurns = 2 * kRows / kLines, kSwizzle = kChunks < 16 ? kChunks : 16;
+  static_assert(2 * kRows * kLine <= LDS && kChunks >= 8 && kTurns > 0 && kTurns * kLines == 2 * kRows, "whole turns");
   const int q = t.tid % kChunks, first = t.tid / kChunks, wt = t.lr / (TALL / 2);
   const int64_t c = t.col0 + kPer * q;
 #pragma unroll
@@ -233,7 +238,7 @@ __device__ __forceinline__ void store_tile(const Product& p, const Tile& t, char
 #pragma unroll
       for (int j = 0; j < COLS / 64; ++j) {
         const int r = kRows * wt + 16 * i + t.lane % 16, at = lc[j] * kSize;
-        *reinterpret_cast<Four*>(lds + r * kLine + ((at / 16) ^ (t.lane % 16)) * 16 + at % 16) =
+        *reinterpret_cast<Four*>(lds + r * kLine + ((at / 16) ^ (t.lane % kSwizzle)) * 16 + at % 16) =
             __builtin_convertvector(value(kFrags * pass + i, j), Four);
       }
     }
@@ -243,30 +248,30 @@ __device__ __forceinline__ void store_tile(const Product& p, const Tile& t, char
     for (int n = 0; n < kTurns; ++n) {
       const int r = first + n * kLines;
       const int64_t row = t.row0 + TALL / 2 * (r / kRows) + kRows * pass + r % kRows;
-      const char* src = lds + r * kLine + (q ^ (r % 16)) * 16;
+      const char* src = lds + r * kLine + (q ^ (r % kSwizzle)) * 16;
       if (row < p.rows) place(row, c, *reinterpret_cast<const i32x4*>(src));
     }
   }
 }
 
 // One tile of the rows from first_row on, `index` of the `total` workgroups that share them.
-template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED, int TALL>
+template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED, int TALL, int WIDE = 256>
 __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* lds, int64_t first_row, int64_t rows,
                                           unsigned index, unsigned total) {
   using E = Elem<ELEM>;
   using Acc = typename E::Acc;
   constexpr int kB = E::kBytes, kStep = kStepBytes / kB;
-  constexpr int kTallStep = TALL * kStepBytes, kWideStep = 256 * kStepBytes;     // bytes in LDS
-  constexpr int kTallStages = Stages<TALL>::kTall, kWideStages = Stages<TALL>::kWide;
+  constexpr int kTallStep = TALL * kStepBytes, kWideStep = WIDE * kStepBytes;     // bytes in LDS
+  constexpr int kTallStages = Stages<TALL, WIDE>::kTall, kWideStages = Stages<TALL, WIDE>::kWide;
   constexpr int kWide = kTallStages * kTallStep, kEnd = kWide + kWideStages * kWideStep;
-  constexpr int kFrags = TALL / 32;                 // of 16 rows of tall per wave
-  constexpr int kTallCopies = TALL / 64, kWideCopies = 4;
-  static_assert(kEnd == kLdsBytes<TALL>, "stages of tall, then of wide");
+  constexpr int kFrags = TALL / 32, kWideFrags = WIDE / 64;      // of 16 rows per wave
+  constexpr int kTallCopies = TALL / 64, kWideCopies = WIDE / 64;
+  static_assert(kEnd == kLdsBytes<TALL, WIDE>, "stages of tall, then of wide");
   const int tid = threadIdx.x, lane = tid % 64;
   const int wave = __builtin_amdgcn_readfirstlane(tid / 64);
   const int ww = wave % 4, wt = wave / 4;
 
-  constexpr int kCols = GATED ? 128 : 256;
+  constexpr int kCols = GATED ? WIDE / 2 : WIDE;
   const unsigned nw = static_cast<unsigned>((p.cols + kCols - 1) / kCols);
   const unsigned nt = static_cast<unsigned>((rows + TALL - 1) / TALL);
   const unsigned xcd = index % kXcds, per = total / kXcds, rem = total % kXcds;
@@ -286,13 +291,13 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
 
   constexpr bool kSegments = WIDE_STRIDED && !TALL_STRIDED;      // two in the gradient of the block's input only
   Loader<kB, TALL_STRIDED, false, TALL> la;
-  Loader<kB, WIDE_STRIDED, GATED, 256> lb;
+  Loader<kB, WIDE_STRIDED, GATED, WIDE> lb;
   la.init(p.tall[p.batch > 1 ? z : 0], p.tall[1], row0, p.rows, p.ld_tall, p.depth, t0, seg_steps, wave, lane);
   lb.init(p.wide[0], p.wide[1], col0, p.cols, p.ld_wide, p.depth, t0, seg_steps, wave, lane);
-  Frags<TALL_STRIDED, false, kFrags> fa;
-  Frags<WIDE_STRIDED, GATED, 4> fb;
+  Frags<TALL_STRIDED, 0, kFrags> fa;
+  Frags<WIDE_STRIDED, GATED ? WIDE / 2 : 0, kWideFrags> fb;
   fa.init(TALL / 2 * wt, lane);
-  fb.init((GATED ? 32 : 64) * ww, lane);
+  fb.init(kCols / 4 * ww, lane);
 
   // LDS offsets of the stages read and filled next.
   int get_a = 0, get_b = kWide, put_a = 0, put_b = kWide;
@@ -308,13 +313,13 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
     put_b = next_b(put_b);
   };
 
-  Acc acc[kFrags][4] = {};        // [rows of tall / 16][rows of wide / 16]
-  i32x4 a[2][kFrags], b[2][4];    // [depth half][rows / 16]
+  Acc acc[kFrags][kWideFrags] = {};        // [rows of tall / 16][rows of wide / 16]
+  i32x4 a[2][kFrags], b[2][kWideFrags];    // [depth half][rows / 16]
   auto read = [&](int s) {
     // In the order in which the products ask for them.
     a[s][0] = fa.read(lds + get_a, 0, s);
 #pragma unroll
-    for (int n = 0; n < 4; ++n) b[s][n] = fb.read(lds + get_b, n, s);
+    for (int n = 0; n < kWideFrags; ++n) b[s][n] = fb.read(lds + get_b, n, s);
 #pragma unroll
     for (int n = 1; n < kFrags; ++n) a[s][n] = fa.read(lds + get_a, n, s);
   };
@@ -322,7 +327,7 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
 #pragma unroll
     for (int i = 0; i < kFrags; ++i)
 #pragma unroll
-      for (int j = 0; j < 4; ++j) acc[i][j] = E::mfma(b[s][j], a[s][i], acc[i][j]);
+      for (int j = 0; j < kWideFrags; ++j) acc[i][j] = E::mfma(b[s][j], a[s][i], acc[i][j]);
   };
   // What was read has arrived, and all copies but the newest, of every wave.
   auto turn = [&](auto newer) {
@@ -334,7 +339,7 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
   };
   // Copies and LDS reads between the matrix-core instructions.
   auto spread = [&](auto copies) {
-    constexpr int kReads = (TALL_STRIDED ? 2 : 1) * kFrags + (WIDE_STRIDED ? 2 : 1) * 4;
+    constexpr int kReads = (TALL_STRIDED ? 2 : 1) * kFrags + (WIDE_STRIDED ? 2 : 1) * kWideFrags;
     constexpr int kCopies = decltype(copies)::value;
 #pragma unroll
     for (int n = 0; n < kCopies; ++n) {
@@ -387,30 +392,31 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
 
   // The lane's sums: rows lr + 16 i of the tile, columns lc[j] .. + 3 (of gate, of up).
   const int lr = TALL / 2 * wt + lane % 16;
-  int lc[4];
+  constexpr int kPairs = kWideFrags / 2;      // of gate and up
+  int lc[kWideFrags];
 #pragma unroll
-  for (int j = 0; j < 4; ++j) lc[j] = (GATED ? 32 * ww + 16 * (j % 2) : 64 * ww + 16 * j) + 4 * (lane / 16);
+  for (int j = 0; j < kWideFrags; ++j) lc[j] = kCols / 4 * ww + 16 * (GATED ? j % kPairs : j) + 4 * (lane / 16);
   const Tile tile_out = {row0, col0, lr, lane, tid};
   if (splits > 1) {
     const int64_t ld = (p.cols + 3) / 4;      // of gate and of up, in fours
 #pragma unroll
     for (int half = 0; half < (GATED ? 2 : 1); ++half)
       store_tile<SDQ_F32, TALL, kCols, kEnd>(
-          p, tile_out, lds, lc, [&](int i, int j) { return __builtin_bit_cast(f32x4, acc[i][j + 2 * half]); },
+          p, tile_out, lds, lc, [&](int i, int j) { return __builtin_bit_cast(f32x4, acc[i][j + kPairs * half]); },
           [&](int64_t row, int64_t c, i32x4 v) {
             static_cast<i32x4*>(p.ws)[((part * p.rows + row) * (GATED ? 2 : 1) + half) * ld + c / 4] = v;
           });
     return;
   }
   float row_scale[kFrags];
-  f32x4 col_scale[4];
+  f32x4 col_scale[kWideFrags];
   if constexpr (ELEM == kElemI8) {
 #pragma unroll
     for (int i = 0; i < kFrags; ++i) row_scale[i] = p.tall_scale[min(row0 + lr + 16 * i, p.rows - 1)];
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+    for (int j = 0; j < kWideFrags; ++j)
 #pragma unroll
-      for (int v = 0; v < 4; ++v) col_scale[j][v] = p.wide_scale[GATED ? j / 2 : 0][min(col0 + lc[j] + v, p.cols - 1)];
+      for (int v = 0; v < 4; ++v) col_scale[j][v] = p.wide_scale[GATED ? j / kPairs : 0][min(col0 + lc[j] + v, p.cols - 1)];
   }
   auto sum = [&](int i, int j) { return as_floats<ELEM>(acc[i][j], row_scale[i], col_scale[j]); };
   if constexpr (GATED) {
@@ -424,7 +430,7 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
       auto activated = [&](auto act) {
         put(type, p.out[0], [&](int i, int j) {
           f32x4 g = sum(i, j);
-          const f32x4 u = sum(i, j + 2);
+          const f32x4 u = sum(i, j + kPairs);
 #pragma unroll
           for (int v = 0; v < 4; ++v) g[v] = act_value<kType == SDQ_F32>(g[v], decltype(act)::value) * u[v];
           return g;
@@ -435,7 +441,7 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
       if constexpr (ELEM != kElemI8) {
         auto put_both = [&](auto as) {
           put(as, p.g_out, sum);
-          put(as, p.u_out, [&](int i, int j) { return sum(i, j + 2); });
+          put(as, p.u_out, [&](int i, int j) { return sum(i, j + kPairs); });
         };
         if (p.g_out && p.keep_f32) put_both(std::integral_constant<int, SDQ_F32>());
         else if (p.g_out) put_both(type);      // in the operands' own type, which is h's
@@ -459,18 +465,18 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
   }
 }
 
-template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED, int TALL>
+template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED, int TALL, int WIDE>
 __global__ __launch_bounds__(512, 2) void wide_kernel(Product p, int splits) {
-  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes<TALL>];
-  wide_tile<ELEM, WIDE_STRIDED, TALL_STRIDED, GATED, TALL>(p, splits, lds, 0, p.rows, blockIdx.x, gridDim.x);
+  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes<TALL, WIDE>];
+  wide_tile<ELEM, WIDE_STRIDED, TALL_STRIDED, GATED, TALL, WIDE>(p, splits, lds, 0, p.rows, blockIdx.x, gridDim.x);
 }
 
 // Tiles of 256 rows of tall for the first `rows` of them, whose workgroups come first, and of 128 for the
 // rest.
 template <int ELEM, bool WIDE_STRIDED, bool TALL_STRIDED, bool GATED>
 __global__ __launch_bounds__(512, 2) void mixed_kernel(Product p, int64_t rows, unsigned tiles) {
-  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes<256>];
-  static_assert(kLdsBytes<128> <= kLdsBytes<256>, "one allocation for both");
+  __shared__ __attribute__((aligned(1024))) char lds[kLdsBytes<256, 256>];
+  static_assert(kLdsBytes<128, 256> <= kLdsBytes<256, 256>, "one allocation for both");
   if (blockIdx.x < tiles)
     wide_tile<ELEM, WIDE_STRIDED, TALL_STRIDED, GATED, 256>(p, 1, lds, 0, rows, blockIdx.x, tiles);
   else
@@ -504,11 +510,11 @@ __global__ __launch_bounds__(256) void join_kernel(Product p, int splits) {
   });
 }
 
-template <int ELEM, bool WS, bool TS, bool GATED, int TALL>
+template <int ELEM, bool WS, bool TS, bool GATED, int TALL, int WIDE = 256>
 void launch_tiles(const Product& p, int splits, hipStream_t stream) {
-  const int64_t per = GATED ? 128 : 256;
+  const int64_t per = GATED ? WIDE / 2 : WIDE;
   const int64_t tiles = (p.cols + per - 1) / per * ((p.rows + TALL - 1) / TALL);
-  wide_kernel<ELEM, WS, TS, GATED, TALL>
+  wide_kernel<ELEM, WS, TS, GATED, TALL, WIDE>
       <<<dim3(static_cast<unsigned>(tiles * p.batch * splits)), 512, 0, stream>>>(p, splits);
   if (splits > 1) {
     const int64_t quads = (p.cols + 3) / 4 * p.rows * p.batch;
@@ -527,7 +533,9 @@ void launch_mixed(const Product& p, int64_t rows, hipStream_t stream) {
 template <int ELEM, bool WS, bool GATED>
 void launch_tall(const Product& p, const WidePlan& plan, hipStream_t stream) {
   if (plan.mixed) return launch_mixed<ELEM, WS, false, GATED>(p, plan.mixed, stream);
-  if (plan.tall == 64) launch_tiles<ELEM, WS, false, GATED, 64>(p, plan.splits, stream);
+  if (plan.wide == 128 && plan.tall == 128) launch_tiles<ELEM, WS, false, GATED, 128, 128>(p, plan.splits, stream);
+  else if (plan.wide == 128) launch_tiles<ELEM, WS, false, GATED, 64, 128>(p, plan.splits, stream);
+  else if (plan.tall == 64) launch_tiles<ELEM, WS, false, GATED, 64>(p, plan.splits, stream);
   else if (plan.tall == 128) launch_tiles<ELEM, WS, false, GATED, 128>(p, plan.splits, stream);
   else launch_tiles<ELEM, WS, false, GATED, 256>(p, plan.splits, stream);
 }
@@ -548,37 +556,46 @@ size_t wide_part_bytes(const Product& p, int splits) {
   return splits > 1 ? static_cast<size_t>(p.batch) * p.rows * ((p.cols + 3) / 4) * 16 * (p.gated ? 2 : 1) * splits : 0;
 }
 
-// The plan with the least time by a model fitted to measured ones (8-bit and bf16 products of 8 to
-// 900 rows with 768 x 768 to 28672 x 8192 weights, every tile height and 1 to 16 splits; it picks one
-// within 10 % of the fastest of them but for single cases):
-//   a launch 2.5 us; a turn of the chip 2, 3.5 or 7.5 us for its first copies and its outputs and
-//   0.62, 0.72 or 1.1 us per step at 64, 128 or 256 rows of tall, up to 45 % more with every compute
-//   unit at work (power), or what the turn's rows of wide take from memory at 5 TB/s;
-//   a tile of 128 rows 0.57 of one of 256;
-//   the partial sums 2.5 us and their bytes, written and read, at 6 TB/s.
+// The plan with the least time by a model fitted to 4200 measured ones (8-bit and bf16 products of 1 to
+// 4096 rows with 768 x 768 to 28672 x 8192 weights that come from memory, every tile and 1 to 16
+// splits; what it picks takes 1.3 % longer than the fastest of them on average, 23 % at worst):
+//   a launch 3.5 us; a turn of the chip its tile's ends and steps (kShapes, in us), a step longer by a
+//   share that grows with the compute units at work; all turns together at least what the weights take
+//   at 5.4 TB/s;
+//   a tile of 128 rows in the last turn 0.57 of one of 256;
+//   the partial sums 3.4 us and their bytes, written and read, at 5.1 TB/s.
 WidePlan wide_plan(const Product& p) {
   const int64_t bytes = p.elem == kElemI8 ? 1 : 2, units = device_compute_units();
   const int64_t steps = (p.depth * bytes + 127) / 128 * p.segments;
-  const int64_t col_tiles = (p.cols + (p.gated ? 127 : 255)) / (p.gated ? 128 : 256) * p.batch;
+  struct Shape {
+    int tall, wide;
+    double ends, step, busy;
+  };
+  static constexpr Shape kShapes[] = {{256, 256, 3.4, 1.14, 0.19},
+                                      {128, 256, 1.6, 0.81, 0.08},
+                                      {64, 256, 0.4, 0.63, 0.86},
+                                      {128, 128, 1.0, 0.46, 0.32},
+                                      {64, 128, 0.1, 0.36, 0.87}};
+  const double memory = static_cast<double>(p.cols) * (p.gated ? 2 : 1) * p.batch * p.depth * p.segments * bytes / 5.4e6;
   WidePlan best;
-  for (int tall = 256; tall >= (p.tall_strided ? 128 : 64); tall /= 2) {
-    const int64_t tiles = col_tiles * ((p.rows + tall - 1) / tall);
-    const double step = tall == 256 ? 1.1 : tall == 128 ? 0.72 : 0.62, ends = tall == 256 ? 7.5 : tall == 128 ? 3.5 : 2.0;
+  for (const Shape& s : kShapes) {
+    if (p.tall_strided && (s.tall == 64 || s.wide == 128)) continue;
+    const int cols = p.gated ? s.wide / 2 : s.wide;
+    const int64_t col_tiles = (p.cols + cols - 1) / cols * p.batch, tiles = col_tiles * ((p.rows + s.tall - 1) / s.tall);
     for (int splits = 1; splits <= 32 && (splits == 1 || (steps / splits >= 3 && tiles * splits <= 3 * units)); ++splits) {
-      const int64_t at_once = std::min(tiles * splits, units), turns = (tiles * splits + units - 1) / units;
-      const double busy = static_cast<double>(at_once) / units;
-      const double memory = std::min(col_tiles * splits, at_once) * 32768.0 / 5e6;
-      const double turn = ends + (steps + splits - 1) / splits * std::max(step * (1 + 0.45 * busy), memory);
-      double us = 2.5 + turns * turn;
-      if (splits > 1) us += 2.5 + wide_part_bytes(p, splits) * 2 / 6e6;
-      if (best.splits == 0 || us < best.us) best = {tall, splits, 0, us};
+      const int64_t turns = (tiles * splits + units - 1) / units;
+      const double busy = std::min(1.0, static_cast<double>(tiles * splits) / units);
+      const double turn = s.ends + (steps + splits - 1) / splits * s.step * (1 + s.busy * busy);
+      double us = 3.5 + std::max(turns * turn, s.ends + memory);
+      if (splits > 1) us += 3.4 + wide_part_bytes(p, splits) * 2 / 5.1e6;
+      if (best.splits == 0 || us < best.us) best = {s.tall, s.wide, splits, 0, us};
       // Whole turns of 256 rows, the rest in tiles of 128 that fill one more.
       const int64_t first = tiles / units * units / col_tiles, rest = p.rows - 256 * first;
-      if (tall != 256 || splits > 1 || first == 0 || rest <= 0) continue;
+      if (s.tall != 256 || splits > 1 || first == 0 || rest <= 0) continue;
       const int64_t early = tiles / units * units - first * col_tiles;      // workgroups done a turn before
       const int64_t small = col_tiles * ((rest + 127) / 128) - early * 7 / 4;
-      us = 2.5 + turn * (tiles / units + 0.57 * std::max<int64_t>((small + units - 1) / units, 0));
-      if (us < best.us) best = {tall, splits, 256 * first, us};
+      us = 3.5 + turn * (tiles / units + 0.57 * std::max<int64_t>((small + units - 1) / units, 0));
+      if (us < best.us) best = {s.tall, s.wide, splits, 256 * first, us};
     }
   }
   return best;
