@@ -67,6 +67,21 @@ size_t product_ws_bytes(const Product& p);
 // is; elements past n are then zeros (depth-contiguous) or anything (strided).
 int64_t product_ld(const Product& p, int64_t n);
 sdq_status launch_product(const Product& p, hipStream_t stream);
+// Copies of matrices of rows of `len` bytes to rows of ld bytes (a multiple of 16), the rest of them zeros.
+struct PadJob {
+  const char* src = nullptr;
+  char* dst = nullptr;
+  int64_t len = 0, ld = 0, chunks = 0;      // chunks: of 16 bytes, in all rows
+  unsigned blocks = 0;                      // workgroups that share them
+};
+struct PadJobs {
+  PadJob of[4];
+  int count = 0;
+  unsigned blocks = 0;      // of all
+};
+// The copies that the product takes instead of operands whose rows do not start aligned, for a caller that
+// makes them itself before launch_product; launch_product makes those that were not taken.
+void take_pads(Product* p, PadJobs* jobs);
 // Whether launch_product quantises the rows of an 8-bit product itself, if given x.
 bool product_quantizes(const Product& p);
 
@@ -86,8 +101,9 @@ sdq_status launch_int8_quantize(const void* x, sdq_dtype xt, int64_t m, int64_t 
                                 float* scales, hipStream_t stream);
 
 // dg = dh u act'(g) and du = dh act(g), [m x f], rounded to dh's type t; g and u of type kt (t or F32);
-// dg and du in rows of ld (a multiple of 8), zeros past f.
+// dg and du in rows of ld (a multiple of 8), zeros past f.  The copies are made in the same launch.
 sdq_status launch_gate_gradient(const void* dh, const void* g, const void* u, sdq_dtype t, sdq_dtype kt, int64_t m,
-                                int64_t f, int64_t ld, int act, void* dg, void* du, hipStream_t stream);
+                                int64_t f, int64_t ld, int act, void* dg, void* du, const PadJobs& pads,
+                                hipStream_t stream);
 
 }  // namespace sdq

@@ -154,7 +154,7 @@ Product weight_gradient(sdq_dtype t, int64_t m, int64_t f, int64_t k) {
 }
 
 struct BackwardSpace {
-  void *dg, *du, *product;
+  void *dg, *du, *dx_product, *dw_product;
   int64_t ld;      // of dg and du
   size_t bytes;
 };
@@ -166,8 +166,8 @@ BackwardSpace backward_space(sdq_dtype t, int64_t m, int64_t f, int64_t k, void*
   const size_t bytes = static_cast<size_t>(m) * s.ld * 2;
   s.dg = c.take(bytes);
   s.du = c.take(bytes);
-  const size_t a = product_ws_bytes(x), b = product_ws_bytes(w);
-  s.product = c.take(a > b ? a : b);
+  s.dx_product = c.take(product_ws_bytes(x));
+  s.dw_product = c.take(product_ws_bytes(w));
   s.bytes = c.off;
   return s;
 }
@@ -292,33 +292,28 @@ sdq_status sdq_gated_linear_backward(const void* dh, const void* x, sdq_dtype t,
   if (st != SDQ_OK) return st;
   const hipStream_t hs = static_cast<hipStream_t>(stream);
   if (!dx && !dgate) return SDQ_OK;
+  Product x_product = input_gradient(t, m, f, k), w_product = weight_gradient(t, m, f, k);
+  x_product.wide[0] = gate;
+  x_product.wide[1] = up;
+  x_product.tall[0] = w_product.tall[0] = s.dg;
+  x_product.tall[1] = w_product.tall[1] = s.du;
+  x_product.out[0] = dx;
+  x_product.ws = s.dx_product;
+  w_product.wide[0] = x;
+  w_product.out[0] = dgate;
+  w_product.out[1] = dup;
+  w_product.accumulate = accumulate != 0;
+  w_product.ws = s.dw_product;
   if (m > 0 && f > 0) {
-    st = launch_gate_gradient(dh, g, u, t, kt, m, f, s.ld, act, s.dg, s.du, hs);
+    PadJobs pads;
+    if (dx) take_pads(&x_product, &pads);
+    if (dgate) take_pads(&w_product, &pads);
+    st = launch_gate_gradient(dh, g, u, t, kt, m, f, s.ld, act, s.dg, s.du, pads, hs);
     if (st != SDQ_OK) return st;
   }
   // Without rows or features the sums are empty: the products write zeros.
-  if (dx && m > 0) {
-    Product p = input_gradient(t, m, f, k);
-    p.wide[0] = gate;
-    p.wide[1] = up;
-    p.tall[0] = s.dg;
-    p.tall[1] = s.du;
-    p.out[0] = dx;
-    p.ws = s.product;
-    st = launch_product(p, hs);
-    if (st != SDQ_OK) return st;
-  }
-  if (dgate && f > 0) {
-    Product p = weight_gradient(t, m, f, k);
-    p.wide[0] = x;
-    p.tall[0] = s.dg;
-    p.tall[1] = s.du;
-    p.out[0] = dgate;
-    p.out[1] = dup;
-    p.accumulate = accumulate != 0;
-    p.ws = s.product;
-    st = launch_product(p, hs);
-  }
+  if (dx && m > 0) st = launch_product(x_product, hs);
+  if (st == SDQ_OK && dgate && f > 0) st = launch_product(w_product, hs);
   return st;
 }
 

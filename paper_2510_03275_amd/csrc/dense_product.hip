@@ -10,17 +10,6 @@
 namespace sdq {
 namespace {
 
-// Up to four matrices of rows of `len` bytes copied to rows of ld bytes (a multiple of 16), the rest of
-// them zeros, in one launch.  A thread writes 16 bytes.
-struct PadJob {
-  const char* src = nullptr;
-  char* dst = nullptr;
-  int64_t len = 0, ld = 0, chunks = 0;      // chunks: of 16 bytes, in all rows
-};
-struct PadJobs {
-  PadJob of[4];
-  int count = 0;
-};
 // o / per and the rest, in 32 bits where that is enough (a 64-bit division is a hundred instructions).
 __device__ inline int64_t divide(int64_t o, int64_t per, int64_t* rest) {
   int64_t q;
@@ -29,10 +18,13 @@ __device__ inline int64_t divide(int64_t o, int64_t per, int64_t* rest) {
   *rest = o - q * per;
   return q;
 }
-__global__ __launch_bounds__(256) void pad_rows_kernel(PadJobs jobs) {
-  const PadJob& job = jobs.of[blockIdx.y];
+// The copies' workgroup `block`: a thread writes 16 bytes at a time.
+__device__ inline void pad_block(const PadJobs& jobs, unsigned block) {
+  int n = 0;
+  while (n + 1 < jobs.count && block >= jobs.of[n].blocks) block -= jobs.of[n++].blocks;
+  const PadJob& job = jobs.of[n];
   const int64_t per = job.ld / 16;
-  for (int64_t o = blockIdx.x * int64_t{256} + threadIdx.x; o < job.chunks; o += gridDim.x * int64_t{256}) {
+  for (int64_t o = block * int64_t{256} + threadIdx.x; o < job.chunks; o += job.blocks * int64_t{256}) {
     int64_t c;
     const int64_t row = divide(o, per, &c);
     c *= 16;
@@ -49,14 +41,17 @@ __global__ __launch_bounds__(256) void pad_rows_kernel(PadJobs jobs) {
     *reinterpret_cast<i32x4*>(job.dst + 16 * o) = v;
   }
 }
+__global__ __launch_bounds__(256) void pad_rows_kernel(PadJobs jobs) { pad_block(jobs, blockIdx.x); }
 
 // dg and du, eight elements of a row per thread; rows of dg and du hold ld elements, those past f zeros.
 // A row's last eight start earlier where eight more would pass its end: both threads find the same values.
-// Bound by memory: 4096 x 11008 bf16 (450 MB) in 81 us, 5.5 TB/s.
+// Workgroups from `blocks` on make the copies.  Bound by memory: 4096 x 11008 bf16 (450 MB) in 78 us, 5.7 TB/s.
 template <class S, class K>
 __global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict__ dh, const K* __restrict__ g,
                                                             const K* __restrict__ u, int64_t m, int64_t f, int64_t ld,
-                                                            int act, S* __restrict__ dg, S* __restrict__ du) {
+                                                            int act, S* __restrict__ dg, S* __restrict__ du,
+                                                            unsigned blocks, PadJobs pads) {
+  if (blockIdx.x >= blocks) return pad_block(pads, blockIdx.x - blocks);
   const int64_t o = blockIdx.x * int64_t{256} + threadIdx.x, per = ld / 8;
   if (o >= m * per) return;
   int64_t c;
@@ -147,15 +142,10 @@ Space product_space(const Product& p, void* ws) {
 
 void add_pad(PadJobs* jobs, const void* src, int64_t rows, int64_t ld, void* dst, int64_t ld_dst, int64_t b) {
   if (rows == 0) return;
-  jobs->of[jobs->count++] = {static_cast<const char*>(src), static_cast<char*>(dst), ld * b, ld_dst * b,
-                             rows * ld_dst * b / 16};
-}
-
-void launch_pads(const PadJobs& jobs, hipStream_t stream) {
-  int64_t most = 0;
-  for (int n = 0; n < jobs.count; ++n) most = std::max(most, jobs.of[n].chunks);
-  if (most == 0) return;
-  pad_rows_kernel<<<dim3(static_cast<unsigned>(std::min<int64_t>((most + 255) / 256, 1 << 16)), jobs.count), 256, 0, stream>>>(jobs);
+  const int64_t chunks = rows * ld_dst * b / 16;
+  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((chunks + 255) / 256, 1 << 16));
+  jobs->of[jobs->count++] = {static_cast<const char*>(src), static_cast<char*>(dst), ld * b, ld_dst * b, chunks, blocks};
+  jobs->blocks += blocks;
 }
 
 }  // namespace
@@ -172,28 +162,33 @@ bool product_quantizes(const Product& p) { return p.few && few_quantizes(p); }
 
 size_t product_ws_bytes(const Product& p) { return p.few ? 0 : product_space(p, nullptr).bytes; }
 
+void take_pads(Product* p, PadJobs* jobs) {
+  if (p->few) return;
+  const Space s = product_space(*p, p->ws);
+  const int64_t b = elem_bytes(*p);
+  for (int i = 0; i < 2; ++i) {
+    if (s.wide[i]) {
+      add_pad(jobs, p->wide[i], p->wide_strided ? p->depth : p->cols, p->ld_wide, s.wide[i], s.ld_wide, b);
+      p->wide[i] = s.wide[i];
+    }
+    if (s.tall[i]) {
+      add_pad(jobs, p->tall[i], p->tall_strided ? p->depth : p->rows, p->ld_tall, s.tall[i], s.ld_tall, b);
+      p->tall[i] = s.tall[i];
+    }
+  }
+  p->ld_wide = s.ld_wide;
+  p->ld_tall = s.ld_tall;
+  p->ws = s.parts;
+}
+
 sdq_status launch_product(const Product& given, hipStream_t stream) {
   Product p = given;
   if (p.few) {
     launch_few(p, stream);
   } else {
-    const Space s = product_space(p, p.ws);
-    const int64_t b = elem_bytes(p);
     PadJobs pads;
-    for (int i = 0; i < 2; ++i) {
-      if (s.wide[i]) {
-        add_pad(&pads, p.wide[i], p.wide_strided ? p.depth : p.cols, p.ld_wide, s.wide[i], s.ld_wide, b);
-        p.wide[i] = s.wide[i];
-      }
-      if (s.tall[i]) {
-        add_pad(&pads, p.tall[i], p.tall_strided ? p.depth : p.rows, p.ld_tall, s.tall[i], s.ld_tall, b);
-        p.tall[i] = s.tall[i];
-      }
-    }
-    launch_pads(pads, stream);
-    p.ld_wide = s.ld_wide;
-    p.ld_tall = s.ld_tall;
-    p.ws = s.parts;
+    take_pads(&p, &pads);
+    if (pads.blocks) pad_rows_kernel<<<dim3(pads.blocks), 256, 0, stream>>>(pads);
     launch_wide(p, stream);
   }
   const hipError_t e = hipGetLastError();
@@ -203,19 +198,21 @@ sdq_status launch_product(const Product& given, hipStream_t stream) {
 namespace {
 template <class S, class K>
 void launch_gate(const void* dh, const void* g, const void* u, int64_t m, int64_t f, int64_t ld, int act, void* dg,
-                 void* du, hipStream_t stream) {
-  gate_gradient_kernel<<<dim3(static_cast<unsigned>((m * (ld / 8) + 255) / 256)), 256, 0, stream>>>(
+                 void* du, const PadJobs& pads, hipStream_t stream) {
+  const unsigned blocks = static_cast<unsigned>((m * (ld / 8) + 255) / 256);
+  gate_gradient_kernel<<<dim3(blocks + pads.blocks), 256, 0, stream>>>(
       static_cast<const S*>(dh), static_cast<const K*>(g), static_cast<const K*>(u), m, f, ld, act, static_cast<S*>(dg),
-      static_cast<S*>(du));
+      static_cast<S*>(du), blocks, pads);
 }
 }  // namespace
 
 sdq_status launch_gate_gradient(const void* dh, const void* g, const void* u, sdq_dtype t, sdq_dtype kt, int64_t m,
-                                int64_t f, int64_t ld, int act, void* dg, void* du, hipStream_t stream) {
-  if (t == SDQ_F16 && kt == SDQ_F32) launch_gate<_Float16, float>(dh, g, u, m, f, ld, act, dg, du, stream);
-  else if (t == SDQ_F16) launch_gate<_Float16, _Float16>(dh, g, u, m, f, ld, act, dg, du, stream);
-  else if (kt == SDQ_F32) launch_gate<__bf16, float>(dh, g, u, m, f, ld, act, dg, du, stream);
-  else launch_gate<__bf16, __bf16>(dh, g, u, m, f, ld, act, dg, du, stream);
+                                int64_t f, int64_t ld, int act, void* dg, void* du, const PadJobs& pads,
+                                hipStream_t stream) {
+  if (t == SDQ_F16 && kt == SDQ_F32) launch_gate<_Float16, float>(dh, g, u, m, f, ld, act, dg, du, pads, stream);
+  else if (t == SDQ_F16) launch_gate<_Float16, _Float16>(dh, g, u, m, f, ld, act, dg, du, pads, stream);
+  else if (kt == SDQ_F32) launch_gate<__bf16, float>(dh, g, u, m, f, ld, act, dg, du, pads, stream);
+  else launch_gate<__bf16, __bf16>(dh, g, u, m, f, ld, act, dg, du, pads, stream);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? SDQ_OK : hip_error(e, "gate gradient launch");
 }
