@@ -71,8 +71,8 @@ sdq_status launch_product(const Product& p, hipStream_t stream);
 struct PadJob {
   const char* src = nullptr;
   char* dst = nullptr;
-  int64_t len = 0, ld = 0, chunks = 0;      // chunks: of 16 bytes, in all rows
-  unsigned blocks = 0;                      // workgroups that share them
+  int64_t len = 0, ld = 0, rows = 0;
+  unsigned blocks = 0;      // workgroups that share them
 };
 struct PadJobs {
   PadJob of[4];

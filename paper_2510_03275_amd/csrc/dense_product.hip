@@ -18,28 +18,34 @@ __device__ inline int64_t divide(int64_t o, int64_t per, int64_t* rest) {
   *rest = o - q * per;
   return q;
 }
-// The copies' workgroup `block`: a thread writes 16 bytes at a time.
+// The copies' workgroup `block`: a thread writes 16 bytes of two rows, whose reads are in flight
+// together.  A row's last bytes come from 16 that end with it, shifted.
+constexpr int kPadRows = 2;
 __device__ inline void pad_block(const PadJobs& jobs, unsigned block) {
   int n = 0;
   while (n + 1 < jobs.count && block >= jobs.of[n].blocks) block -= jobs.of[n++].blocks;
-  const PadJob& job = jobs.of[n];
-  const int64_t per = job.ld / 16;
-  for (int64_t o = block * int64_t{256} + threadIdx.x; o < job.chunks; o += job.blocks * int64_t{256}) {
-    int64_t c;
-    const int64_t row = divide(o, per, &c);
-    c *= 16;
-    const char* at = job.src + row * job.len + c;
-    i32x4 v = {0, 0, 0, 0};
-    if (c + 16 <= job.len) {
-      __builtin_memcpy(&v, at, 16);
-    } else {
-      char e[16];
+  const PadJob job = jobs.of[n];
+  const int64_t per = job.ld / 16, step = (job.rows + kPadRows - 1) / kPadRows;
+  int64_t c;
+  const int64_t row = divide(block * int64_t{256} + threadIdx.x, per, &c);
+  c *= 16;
+  if (row >= step) return;
+  const int64_t from = max(min(c, job.len - 16), int64_t{0});
+  unsigned __int128 v[kPadRows] = {};
 #pragma unroll
-      for (int j = 0; j < 16; ++j) e[j] = c + j < job.len ? at[j] : char(0);
-      __builtin_memcpy(&v, e, 16);
+  for (int i = 0; i < kPadRows; ++i) {
+    const char* src = job.src + min(row + i * step, job.rows - 1) * job.len;
+    if (c < job.len && job.len >= 16) {
+      __builtin_memcpy(&v[i], src + from, 16);
+    } else if (c < job.len) {
+      for (int j = 0; j < static_cast<int>(job.len); ++j)
+        v[i] |= static_cast<unsigned __int128>(static_cast<unsigned char>(src[j])) << 8 * j;
     }
-    *reinterpret_cast<i32x4*>(job.dst + 16 * o) = v;
   }
+#pragma unroll
+  for (int i = 0; i < kPadRows; ++i)
+    if (row + i * step < job.rows)
+      *reinterpret_cast<unsigned __int128*>(job.dst + (row + i * step) * job.ld + c) = v[i] >> 8 * static_cast<int>(c - from) % 128;
 }
 __global__ __launch_bounds__(256) void pad_rows_kernel(PadJobs jobs) { pad_block(jobs, blockIdx.x); }
 
@@ -57,6 +63,10 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict_
   int64_t c;
   const int64_t row = divide(o, per, &c), n = f < 8 ? f : 8;
   c *= 8;
+  if (c >= f) {      // rows of dg and du start aligned
+    *reinterpret_cast<i32x4*>(dg + 8 * o) = *reinterpret_cast<i32x4*>(du + 8 * o) = i32x4{0, 0, 0, 0};
+    return;
+  }
   const bool last = c + 8 >= f;
   c = last ? f - n : c;
   const int64_t i = row * f + c, at = row * ld + c;
@@ -93,11 +103,15 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict_
       }
   }
   if (last)
-    for (int64_t z = row * ld + f; z < (row + 1) * ld; ++z) dg[z] = du[z] = S(0);
+    for (int64_t z = row * ld + f; z < 8 * (o + 1); ++z) dg[z] = du[z] = S(0);
 }
 
 int64_t elem_bytes(const Product& p) { return p.elem == kElemI8 ? 1 : 2; }
-int64_t aligned_ld(const Product& p, int64_t ld) { return static_cast<int64_t>(align_up(ld * elem_bytes(p), 16)) / elem_bytes(p); }
+// Rows of n elements at whole 128-byte lines: a step of 128 bytes then reads one line of a row, not two
+// (fp16 777 x 1008 against gate and up of 2736 takes 16.4 us, 777 x 1024 15.5).
+int64_t line_ld(const Product& p, int64_t n) { return static_cast<int64_t>(align_up(n * elem_bytes(p), 128)) / elem_bytes(p); }
+// Of an operand's rows, or of their copies if they do not start 16-byte aligned.
+int64_t aligned_ld(const Product& p, int64_t ld) { return ld * elem_bytes(p) % 16 ? line_ld(p, ld) : ld; }
 
 // Up to 64 rows the faster kernel by their models (8-bit: 768 x 768 weights 3 us at one row against 7
 // on tiles, 4096 x 11008 16 against 19 at 8 rows and 30 against 20 at 24; bf16 gate and up of 28672 x
@@ -142,9 +156,9 @@ Space product_space(const Product& p, void* ws) {
 
 void add_pad(PadJobs* jobs, const void* src, int64_t rows, int64_t ld, void* dst, int64_t ld_dst, int64_t b) {
   if (rows == 0) return;
-  const int64_t chunks = rows * ld_dst * b / 16;
-  const unsigned blocks = static_cast<unsigned>(std::min<int64_t>((chunks + 255) / 256, 1 << 16));
-  jobs->of[jobs->count++] = {static_cast<const char*>(src), static_cast<char*>(dst), ld * b, ld_dst * b, chunks, blocks};
+  const int64_t threads = (rows + kPadRows - 1) / kPadRows * (ld_dst * b / 16);
+  const unsigned blocks = static_cast<unsigned>((threads + 255) / 256);
+  jobs->of[jobs->count++] = {static_cast<const char*>(src), static_cast<char*>(dst), ld * b, ld_dst * b, rows, blocks};
   jobs->blocks += blocks;
 }
 
@@ -156,7 +170,7 @@ void plan_product(Product* p) {
   p->few = takes_few(*p);
 }
 
-int64_t product_ld(const Product& p, int64_t n) { return p.few ? n : aligned_ld(p, n); }
+int64_t product_ld(const Product& p, int64_t n) { return p.few ? n : line_ld(p, n); }
 
 bool product_quantizes(const Product& p) { return p.few && few_quantizes(p); }
 

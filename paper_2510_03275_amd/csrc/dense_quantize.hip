@@ -81,7 +81,7 @@ __global__ __launch_bounds__(T == 64 ? 256 : T) void quantize_rows_kernel(const 
 #pragma unroll
     for (int j = 0; j < CHUNKS; ++j) store(tid + T * j, v[j]);
     for (int64_t c = tid + T * CHUNKS; c < chunks; c += T) store(c, load(c));
-    if (k + tid < ld) dst[k + tid] = 0;      // ld - k < 16
+    for (int64_t c = k + tid; c < ld; c += T) dst[c] = 0;
     if (T > 64) __syncthreads();             // part is read before the next row's
   }
 }
