@@ -113,9 +113,9 @@ int64_t line_ld(const Product& p, int64_t n) { return static_cast<int64_t>(align
 // Of an operand's rows, or of their copies if they do not start 16-byte aligned.
 int64_t aligned_ld(const Product& p, int64_t ld) { return ld * elem_bytes(p) % 16 ? line_ld(p, ld) : ld; }
 
-// Up to 64 rows the faster kernel by their models (8-bit: 768 x 768 weights 3 us at one row against 7
-// on tiles, 4096 x 11008 16 against 19 at 8 rows and 30 against 20 at 24; bf16 gate and up of 28672 x
-// 8192 232 against 198 at 12 rows); the few-row one for rows that do not start aligned, which it takes
+// Up to 64 rows the faster kernel by their models (weights from memory, 8-bit: 768 x 768 2.9 us at one
+// row against 5.3 on tiles, 4096 x 11008 14 against 16 at 8 rows and 30 against 16 at 32; bf16 gate and up
+// of 28672 x 8192 177 against 162 at 8 rows); the few-row one for rows that do not start aligned, which it takes
 // as they are.
 bool takes_few(const Product& p) {
   if (p.wide_strided || p.rows > 64) return false;

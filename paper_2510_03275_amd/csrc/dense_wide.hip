@@ -5,10 +5,10 @@
 // cores of a SIMD for 2048 clocks; beside it go 192 KB of LDS reads (768 clocks), 64 KB
 // of copies from L2 and the waits of a barrier.  Measured on bf16 2048 x (2 x 28672) x 8192:
 // the matrix cores work 80 % of 2.3 M clocks, no LDS bank conflicts, and random data
-// brings the clock down to 1.78 GHz (power), so what an instruction costs in energy counts
-// as much as what it hides: 1.35-1.42 PFLOP/s fused with its activation, where a library's plain
-// product of the same size reaches 1.41-1.46 on the same boxes; 8-bit 4096 x 28672 x 8192
-// 2.5-2.7 POP/s (library 2.3).
+// brings the clock down to 1.75 GHz (power), so what an instruction costs in energy counts
+// as much as what it hides: 1.38-1.43 PFLOP/s fused with its activation, where a library's plain
+// product of the same size reaches 1.41-1.46 on the same cards; 8-bit 4096 x 28672 x 8192
+// 2.6-2.7 POP/s (library 2.3; 3.4 on operands of zeros).
 //
 //   tile      Eight waves, two to a SIMD; wave (wt, ww) forms half the rows of tall by
 //             64 of wide with 16 x 16 matrix instructions (128 x 64 in 128 registers).  (Four waves of
