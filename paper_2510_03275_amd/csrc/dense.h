@@ -93,6 +93,7 @@ double few_us(const Product& p);      // about what it takes
 // Tiles of 256 rows of wide, rows aligned (dense_wide.hip); the sums of a depth in parts take
 // wide_part_bytes of the workspace.
 WidePlan wide_plan(const Product& p);
+double wide_least_us(const Product& p);      // no plan's time is less
 size_t wide_part_bytes(const Product& p, int splits);
 void launch_wide(const Product& p, hipStream_t stream);
 

@@ -109,7 +109,11 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(const S* __restrict_
 int64_t elem_bytes(const Product& p) { return p.elem == kElemI8 ? 1 : 2; }
 // Rows of n elements at whole 128-byte lines: a step of 128 bytes then reads one line of a row, not two
 // (fp16 777 x 1008 against gate and up of 2736 takes 16.4 us, 777 x 1024 15.5).
-int64_t line_ld(const Product& p, int64_t n) { return static_cast<int64_t>(align_up(n * elem_bytes(p), 128)) / elem_bytes(p); }
+// The longest rows keep to 16 bytes: 256 of them are addressed with 31 bits.
+int64_t line_ld(const Product& p, int64_t n) {
+  const int64_t b = elem_bytes(p), bytes = n * b;
+  return static_cast<int64_t>(align_up(bytes, bytes > (1 << 23) - 128 ? 16 : 128)) / b;
+}
 // Of an operand's rows, or of their copies if they do not start 16-byte aligned.
 int64_t aligned_ld(const Product& p, int64_t ld) { return ld * elem_bytes(p) % 16 ? line_ld(p, ld) : ld; }
 
@@ -117,10 +121,15 @@ int64_t aligned_ld(const Product& p, int64_t ld) { return ld * elem_bytes(p) % 1
 // row against 5.3 on tiles, 4096 x 11008 14 against 16 at 8 rows and 30 against 16 at 32; bf16 gate and up
 // of 28672 x 8192 177 against 162 at 8 rows); the few-row one for rows that do not start aligned, which it takes
 // as they are.
-bool takes_few(const Product& p) {
-  if (p.wide_strided || p.rows > 64) return false;
-  const int64_t b = elem_bytes(p);
-  return p.ld_wide * b % 16 || p.ld_tall * b % 16 || few_us(p) < p.plan.us;
+// Where the tiles' least possible time is more, they are not planned (0.4 us of the host).
+bool takes_few(Product* p) {
+  const bool can = !p->wide_strided && p->rows <= 64;
+  const int64_t b = elem_bytes(*p);
+  if (can && (p->ld_wide * b % 16 || p->ld_tall * b % 16)) return true;
+  const double us = can ? few_us(*p) : 0;
+  if (can && us < wide_least_us(*p)) return true;
+  p->plan = wide_plan(*p);
+  return can && us < p->plan.us;
 }
 
 // Workspace of a product on tiles: copies of the operands whose rows do not start aligned, then
@@ -166,8 +175,7 @@ void add_pad(PadJobs* jobs, const void* src, int64_t rows, int64_t ld, void* dst
 
 void plan_product(Product* p) {
   if (p->rows == 0 || p->cols == 0) return;      // nothing is launched
-  p->plan = wide_plan(*p);
-  p->few = takes_few(*p);
+  p->few = takes_few(p);
 }
 
 int64_t product_ld(const Product& p, int64_t n) { return p.few ? n : line_ld(p, n); }

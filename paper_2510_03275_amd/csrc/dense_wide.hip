@@ -564,7 +564,11 @@ size_t wide_part_bytes(const Product& p, int splits) {
 //   at 5.4 TB/s;
 //   a tile of 128 rows in the last turn 0.57 of one of 256;
 //   the partial sums 3.4 us and their bytes, written and read, at 5.1 TB/s.
+double wide_least_us(const Product& p) {
+  return 3.5 + static_cast<double>(p.cols) * (p.gated ? 2 : 1) * p.batch * p.depth * p.segments * (p.elem == kElemI8 ? 1 : 2) / 5.4e6;
+}
 WidePlan wide_plan(const Product& p) {
+  const double least = wide_least_us(p);
   const int64_t bytes = p.elem == kElemI8 ? 1 : 2, units = device_compute_units();
   const int64_t steps = (p.depth * bytes + 127) / 128 * p.segments;
   struct Shape {
@@ -576,7 +580,6 @@ WidePlan wide_plan(const Product& p) {
                                       {64, 256, 0.4, 0.63, 0.86},
                                       {128, 128, 1.0, 0.46, 0.32},
                                       {64, 128, 0.1, 0.36, 0.87}};
-  const double memory = static_cast<double>(p.cols) * (p.gated ? 2 : 1) * p.batch * p.depth * p.segments * bytes / 5.4e6;
   WidePlan best;
   for (const Shape& s : kShapes) {
     if (p.tall_strided && (s.tall == 64 || s.wide == 128)) continue;
@@ -586,7 +589,7 @@ WidePlan wide_plan(const Product& p) {
       const int64_t turns = (tiles * splits + units - 1) / units;
       const double busy = std::min(1.0, static_cast<double>(tiles * splits) / units);
       const double turn = s.ends + (steps + splits - 1) / splits * s.step * (1 + s.busy * busy);
-      double us = 3.5 + std::max(turns * turn, s.ends + memory);
+      double us = std::max(3.5 + turns * turn, least + s.ends);
       if (splits > 1) us += 3.4 + wide_part_bytes(p, splits) * 2 / 5.1e6;
       if (best.splits == 0 || us < best.us) best = {s.tall, s.wide, splits, 0, us};
       // Whole turns of 256 rows, the rest in tiles of 128 that fill one more.
