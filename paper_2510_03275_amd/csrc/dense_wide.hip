@@ -408,8 +408,8 @@ __device__ __forceinline__ void wide_tile(const Product& p, int splits, char* ld
           });
     return;
   }
-  float row_scale[kFrags];
-  f32x4 col_scale[kWideFrags];
+  float row_scale[kFrags] = {};
+  f32x4 col_scale[kWideFrags] = {};
   if constexpr (ELEM == kElemI8) {
 #pragma unroll
     for (int i = 0; i < kFrags; ++i) row_scale[i] = p.tall_scale[min(row0 + lr + 16 * i, p.rows - 1)];
@@ -556,6 +556,12 @@ size_t wide_part_bytes(const Product& p, int splits) {
   return splits > 1 ? static_cast<size_t>(p.batch) * p.rows * ((p.cols + 3) / 4) * 16 * (p.gated ? 2 : 1) * splits : 0;
 }
 
+// What any plan takes at least by the model below: its launch and the weights' stream.
+double wide_least_us(const Product& p) {
+  const double bytes = (p.elem == kElemI8 ? 1.0 : 2.0) * p.depth * p.segments * p.cols * p.batch * (p.gated ? 2 : 1);
+  return 3.5 + bytes / 5.4e6;
+}
+
 // The plan with the least time by a model fitted to 4200 measured ones (8-bit and bf16 products of 1 to
 // 4096 rows with 768 x 768 to 28672 x 8192 weights that come from memory, every tile and 1 to 16
 // splits; what it picks takes 1.3 % longer than the fastest of them on average, 23 % at worst):
@@ -564,9 +570,6 @@ size_t wide_part_bytes(const Product& p, int splits) {
 //   at 5.4 TB/s;
 //   a tile of 128 rows in the last turn 0.57 of one of 256;
 //   the partial sums 3.4 us and their bytes, written and read, at 5.1 TB/s.
-double wide_least_us(const Product& p) {
-  return 3.5 + static_cast<double>(p.cols) * (p.gated ? 2 : 1) * p.batch * p.depth * p.segments * (p.elem == kElemI8 ? 1 : 2) / 5.4e6;
-}
 WidePlan wide_plan(const Product& p) {
   const double least = wide_least_us(p);
   const int64_t bytes = p.elem == kElemI8 ? 1 : 2, units = device_compute_units();
